@@ -406,6 +406,99 @@ int ann_score_pairs_noalloc(const ann_graph *g, const ann_mlp *m, const void *qu
                             void *stream);
 
 /*
+ * ---- The block of a projector ----
+ * The vectors a search works on are the outputs of two networks, the user and the item projector H_u and H_v
+ * (Sec. 2.2 step 1, Sec. 3.1).  The entry points below are the operators of a pre-norm residual block of such a network,
+ *     y = x + dropout(ffn(layer_norm(x))),
+ * for serving and, with their gradients, for training.  Rows are vectors of a batch; `dtype` is ANN_F32, ANN_BF16 or
+ * ANN_F16 and is the type of the rows, of the parameters and of their gradients.  Sums and statistics are formed in
+ * fp32, in an order that depends on the sizes and the alignment only: a call repeated gives the same bits.  Row strides ld_* are
+ * in elements, >= the row's width; arrays without a stride are dense.  Pointers need the alignment of their elements only, a
+ * workspace 256 bytes.  Gradients are written, not added to.  Every call only enqueues kernels on `stream`, allocates
+ * nothing and can be recorded into a HIP graph.  Calls that share a workspace must not overlap in time.
+ */
+
+/*
+ * Layer norm: out[r][c] = (x[r][c] - mean_r) * rstd_r * gamma[c] + beta[c], mean_r the mean of row r,
+ * rstd_r = 1 / sqrt(mean of (x[r][c] - mean_r)^2 + eps).
+ *   x_dev [M][d], out_dev [M][d] : may be the same array with the same stride
+ *   gamma_dev, beta_dev [d]      : NULL = ones, zeros
+ *   mean_dev, rstd_dev [M] fp32  : written for the gradient; NULL where none is taken
+ * M >= 0 (0: nothing is done), 1 <= d <= 2^24, eps >= 0 and finite.
+ */
+int ann_layer_norm(const void *x_dev, int64_t ld_x, const void *gamma_dev, const void *beta_dev, int64_t M, int32_t d,
+                   int32_t dtype, double eps, void *out_dev, int64_t ld_out, float *mean_dev, float *rstd_dev,
+                   void *stream);
+
+/*
+ * Its gradient: with g = dout * gamma and xh = (x - mean) * rstd,
+ *     dx = rstd * (g - mean over the row of g - xh * mean over the row of g * xh),
+ *     dgamma = sum over the rows of dout * xh, dbeta = sum over the rows of dout.
+ * dout_dev [M][d]; x_dev, gamma_dev, mean_dev, rstd_dev as in the forward call.  dx_dev [M][d] may be dout_dev or x_dev;
+ * dx_dev, dgamma_dev, dbeta_dev: NULL = not wanted.  With M = 0 dgamma and dbeta are zeroed.
+ * workspace_dev: ann_layer_norm_backward_workspace_bytes(M, d, dtype) bytes (0 on invalid arguments; may be NULL where
+ * neither dgamma nor dbeta is wanted).
+ */
+size_t ann_layer_norm_backward_workspace_bytes(int64_t M, int32_t d, int32_t dtype);
+int ann_layer_norm_backward(const void *dout_dev, int64_t ld_dout, const void *x_dev, int64_t ld_x,
+                            const void *gamma_dev, const float *mean_dev, const float *rstd_dev, int64_t M, int32_t d,
+                            int32_t dtype, void *dx_dev, int64_t ld_dx, void *dgamma_dev, void *dbeta_dev,
+                            void *workspace_dev, size_t workspace_bytes, void *stream);
+
+/*
+ * Dropout: out[e] = residual[e] + (kept(e) ? x[e] * scale : 0), formed in fp32 and rounded once.  The choice is a pure function
+ * of (seed, draw, e), so no mask is stored: the gradient of x is this call on dout with the same seed and draw and no residual.
+ * Philox4x32-10 with counter (e / 8, draw) and key (seed low half, seed high half ^ 0x64726F70; the constant keeps the
+ * words apart from those of ann_users_add_noise) gives four words, their halves, low first, eight 16-bit numbers;
+ * element e is kept iff number e % 8 is >= t, t = round(65536 * p), and scale = 65536 / (65536 - t): p is taken to the
+ * nearest 2^-16 and the mean is exact for that probability.  p = 0 keeps, p = 1 drops everything.  What a dropped element
+ * holds does not matter (infinities, NaN).
+ *   x_dev, residual_dev, out_dev [n] : residual_dev NULL = none; out_dev may be x_dev or residual_dev
+ *   draw_dev                         : NULL, or one uint64 on the device that is added to `draw` when the kernel runs,
+ *                                      so that the replays of a recorded call can draw anew
+ */
+int ann_dropout(const void *x_dev, const void *residual_dev, void *out_dev, int64_t n, int32_t dtype, double p,
+                uint64_t seed, uint64_t draw, const uint64_t *draw_dev, void *stream);
+
+/*
+ * Gated feed-forward block: [gate | up] = x w_in^T + b_in, h = act(gate) * up, out = h w_out^T + b_out.
+ *   x_dev     [M][d_in], out_dev [M][d_out] : must not overlap
+ *   w_in_dev  [2 * d_hidden][d_in]          : the rows of the gate, then those of the up projection (row = one output unit)
+ *   w_out_dev [d_out][d_hidden]
+ *   b_in_dev  [2 * d_hidden], b_out_dev [d_out] : NULL = none
+ *   act       : ANN_SILU z * sigmoid(z), ANN_GELU z * Phi(z) (the normal distribution function, not its tanh form),
+ *               ANN_SIGMOID, ANN_RELU
+ *   pre_dev   [M][2 * d_hidden] fp32          : gate and up before the activation, written for the gradient; NULL where none is taken
+ * Products are accumulated in fp32.  In the 16-bit types h is rounded to the type, as the operand of the second product;
+ * gate and up are not rounded.  fp16 overflows where the formula's h or out do.
+ * M >= 0 (0: nothing is done), M < 2^31; every width 1 .. 2^20.
+ * workspace_dev: ann_gated_ffn_workspace_bytes with the same sizes (0 on invalid ones).
+ */
+enum { ANN_SILU = 0, ANN_GELU = 1, ANN_SIGMOID = 2, ANN_RELU = 3 };
+size_t ann_gated_ffn_workspace_bytes(int64_t M, int32_t d_in, int32_t d_hidden, int32_t d_out, int32_t dtype);
+int ann_gated_ffn(const void *x_dev, int64_t ld_x, const void *w_in_dev, const void *b_in_dev, const void *w_out_dev,
+                  const void *b_out_dev, int64_t M, int32_t d_in, int32_t d_hidden, int32_t d_out, int32_t act,
+                  int32_t dtype, void *out_dev, int64_t ld_out, float *pre_dev, void *workspace_dev,
+                  size_t workspace_bytes, void *stream);
+
+/*
+ * Its gradient, with (gate, up) = pre as the forward call wrote it, h = act(gate) * up:
+ *     dh = dout w_out, dgate = dh * up * act'(gate), dup = dh * act(gate), dx = [dgate | dup] w_in,
+ *     dw_in = [dgate | dup]^T x, dw_out = dout^T h, db_in = column sums of [dgate | dup], db_out = column sums of dout.
+ * In the 16-bit types dgate, dup and h are rounded to the type, as operands of the products (and db_in sums the rounded
+ * values); nothing else is rounded before the results.  ANN_RELU has slope 0 at 0.
+ * dout_dev [M][d_out]; dx_dev [M][d_in] must not overlap dout_dev or x_dev; dx_dev, dw_in_dev, db_in_dev, dw_out_dev,
+ * db_out_dev have the shapes of what they are gradients of, NULL = not wanted.  With M = 0 the parameters' gradients are zeroed.
+ * workspace_dev: ann_gated_ffn_backward_workspace_bytes with the same sizes (0 on invalid ones).
+ */
+size_t ann_gated_ffn_backward_workspace_bytes(int64_t M, int32_t d_in, int32_t d_hidden, int32_t d_out, int32_t dtype);
+int ann_gated_ffn_backward(const void *dout_dev, int64_t ld_dout, const void *x_dev, int64_t ld_x, const float *pre_dev,
+                           const void *w_in_dev, const void *w_out_dev, int64_t M, int32_t d_in, int32_t d_hidden,
+                           int32_t d_out, int32_t act, int32_t dtype, void *dx_dev, int64_t ld_dx, void *dw_in_dev,
+                           void *db_in_dev, void *dw_out_dev, void *db_out_dev, void *workspace_dev,
+                           size_t workspace_bytes, void *stream);
+
+/*
  * Searches that run until every query has converged (ann_search / ann_search_layers with max_iters = 0,
  * ann_search_stream) follow the progress their kernels report to pinned host memory: every round of the batch, and
  * where the search of a small batch, or that of the last queries of a large one, is a single launch, after the first

@@ -12,6 +12,7 @@ import torch
 ANN_OK, ANN_EINVAL, ANN_ENOMEM, ANN_EDEVICE, ANN_ENOTIMPL, ANN_EWORKSPACE = 0, -1, -2, -3, -4, -5
 ANN_F32, ANN_BF16, ANN_F8, ANN_F16 = 0, 1, 2, 3
 ANN_VALIDATE, ANN_MLP_GENERIC = 1, 2
+ANN_SILU, ANN_GELU, ANN_SIGMOID, ANN_RELU = 0, 1, 2, 3
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 # GMPGR_ANN_LIB names another build of the same library (measurement builds with other tuning constants)
@@ -24,6 +25,8 @@ EXPORTS = [
     "ann_search_layers", "ann_search_walkers_workspace_bytes", "ann_search_walkers",
     "ann_search_stream_workspace_bytes", "ann_search_stream", "ann_stream_open", "ann_stream_submit", "ann_stream_step",
     "ann_stream_drain", "ann_stream_close", "ann_score_pairs", "ann_score_pairs_noalloc", "ann_graph_set_locality", "ann_search_visited_set_is_bitmap", "ann_brute_force", "ann_brute_force_workspace_bytes", "ann_rerank", "ann_rerank_workspace_bytes", "ann_users_add_noise", "ann_quantize_e4m3",
+    "ann_layer_norm", "ann_layer_norm_backward_workspace_bytes", "ann_layer_norm_backward", "ann_dropout",
+    "ann_gated_ffn_workspace_bytes", "ann_gated_ffn", "ann_gated_ffn_backward_workspace_bytes", "ann_gated_ffn_backward",
     "ann_search_stats", "ann_set_progress_timeout", "ann_profile_enable", "ann_profile_read", "ann_profile_copy", "ann_last_error",
 ]
 
@@ -116,6 +119,24 @@ def load_library():
     lib.ann_users_add_noise.restype = ctypes.c_int
     lib.ann_quantize_e4m3.argtypes = [vp, i32, i64, ctypes.c_float, vp, vp]
     lib.ann_quantize_e4m3.restype = ctypes.c_int
+    f64, u64 = ctypes.c_double, ctypes.c_uint64
+    lib.ann_layer_norm.argtypes = [vp, i64, vp, vp, i64, i32, i32, f64, vp, i64, vp, vp, vp]
+    lib.ann_layer_norm.restype = ctypes.c_int
+    lib.ann_layer_norm_backward_workspace_bytes.argtypes = [i64, i32, i32]
+    lib.ann_layer_norm_backward_workspace_bytes.restype = sz
+    lib.ann_layer_norm_backward.argtypes = [vp, i64, vp, i64, vp, vp, vp, i64, i32, i32, vp, i64, vp, vp, vp, sz, vp]
+    lib.ann_layer_norm_backward.restype = ctypes.c_int
+    lib.ann_dropout.argtypes = [vp, vp, vp, i64, i32, f64, u64, u64, vp, vp]
+    lib.ann_dropout.restype = ctypes.c_int
+    lib.ann_gated_ffn_workspace_bytes.argtypes = [i64, i32, i32, i32, i32]
+    lib.ann_gated_ffn_workspace_bytes.restype = sz
+    lib.ann_gated_ffn.argtypes = [vp, i64, vp, vp, vp, vp, i64, i32, i32, i32, i32, i32, vp, i64, vp, vp, sz, vp]
+    lib.ann_gated_ffn.restype = ctypes.c_int
+    lib.ann_gated_ffn_backward_workspace_bytes.argtypes = [i64, i32, i32, i32, i32]
+    lib.ann_gated_ffn_backward_workspace_bytes.restype = sz
+    lib.ann_gated_ffn_backward.argtypes = [vp, i64, vp, i64, vp, vp, vp, i64, i32, i32, i32, i32, i32, vp, i64, vp, vp, vp,
+                                           vp, vp, sz, vp]
+    lib.ann_gated_ffn_backward.restype = ctypes.c_int
     lib.ann_search_stats.argtypes = [vp, ctypes.POINTER(Stats), vp]
     lib.ann_search_stats.restype = ctypes.c_int
     lib.ann_set_progress_timeout.argtypes = [ctypes.c_double]
@@ -624,6 +645,248 @@ def ann_quantize_e4m3(src: torch.Tensor, scale: float = 1.0, out: Optional[torch
     _check(load_library().ann_quantize_e4m3(_dev_ptr(src, "src") if n else None, code, n, float(scale),
                                             _dev_ptr(out, "out") if n else None, _stream_ptr(stream)))
     return out
+
+
+# ---- the block of a projector: y = x + dropout(ffn(layer_norm(x))) ----
+#
+# Tensors of one call lie on one device; the call goes to that device's current stream, or to `stream`, a stream of it.
+# Results and workspaces that the call makes belong to the stream it goes to.
+
+_ROW_CODE = {torch.float32: ANN_F32, torch.bfloat16: ANN_BF16, torch.float16: ANN_F16}
+
+
+def _row_code(t: torch.Tensor, name: str) -> int:
+    code = _ROW_CODE.get(t.dtype)
+    if code is None:
+        raise TypeError(f"{name} must be fp32, bf16 or fp16, got {t.dtype}")
+    return code
+
+
+def _row_shape(t: torch.Tensor, name: str):
+    """(rows, width, row stride) of a [..., width] tensor: dense, or [rows][width] whose rows are."""
+    if t.dim() < 1 or t.shape[-1] < 1:
+        raise ValueError(f"{name} must be [..., width] with a width of at least 1, got {tuple(t.shape)}")
+    d = t.shape[-1]
+    if t.is_contiguous():
+        return t.numel() // d, d, d
+    if t.dim() == 2 and t.stride(1) == 1 and t.stride(0) >= d:
+        return t.shape[0], d, t.stride(0)
+    raise ValueError(f"{name} must be contiguous, or [rows][width] with contiguous rows; strides {t.stride()}")
+
+
+def _like(t: torch.Tensor, name: str, x: torch.Tensor, shape, dtype=None) -> None:
+    """t must have this shape, x's device and type (or `dtype`)."""
+    if t.shape != shape:
+        raise ValueError(f"{name} must be {tuple(shape)}, got {tuple(t.shape)}")
+    if t.dtype != (dtype or x.dtype):
+        raise TypeError(f"{name} must be {dtype or x.dtype}, got {t.dtype}")
+    if t.device != x.device:
+        raise ValueError(f"{name} is on {t.device}, the rows are on {x.device}")
+
+
+def _dense(t: Optional[torch.Tensor], name: str, x: torch.Tensor, shape, dtype=None) -> Optional[int]:
+    if t is None:
+        return None
+    _like(t, name, x, shape, dtype)
+    if not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+    return t.data_ptr()
+
+
+class _Here:
+    """The current device and stream are the call's."""
+
+    def __enter__(self):
+        return None
+
+    def __exit__(self, *a):
+        return False
+
+
+_HERE_ALREADY = _Here()
+
+
+def _place(x: torch.Tensor, stream):
+    """What makes x's device, and `stream` where one is given, the current ones while a call allocates and launches."""
+    if not x.is_cuda:
+        raise ValueError("the rows must be a device tensor")
+    if stream is not None:
+        if stream.device != x.device:
+            raise ValueError(f"stream is on {stream.device}, the rows are on {x.device}")
+        return torch.cuda.stream(stream)
+    return _HERE_ALREADY if torch.cuda.current_device() == x.device.index else torch.cuda.device(x.device)
+
+
+def _row_workspace(workspace: Optional[torch.Tensor], need: int, x: torch.Tensor):
+    """(pointer, bytes) of the caller's workspace or of a fresh one, and the tensor that keeps it."""
+    if need == 0:
+        raise AnnError(ANN_EINVAL, ann_last_error())
+    if workspace is None:
+        workspace = torch.empty(need, dtype=torch.uint8, device=x.device)
+    elif workspace.device != x.device or workspace.dtype != torch.uint8 or not workspace.is_contiguous():
+        raise ValueError(f"workspace must be a contiguous uint8 tensor on {x.device}")
+    return workspace
+
+
+def ann_layer_norm(x: torch.Tensor, gamma: Optional[torch.Tensor] = None, beta: Optional[torch.Tensor] = None,
+                   eps: float = 1e-5, save: bool = False, out: Optional[torch.Tensor] = None, stream=None):
+    """Layer norm over the last dimension of x [..., d]; gamma, beta [d] of x's type (None = ones, zeros).  `out` may be
+    x.  With save=True (out, mean, rstd), the last two fp32 [rows], for ann_layer_norm_backward."""
+    code = _row_code(x, "x")
+    M, d, ld = _row_shape(x, "x")
+    gp, bp = _dense(gamma, "gamma", x, (d,)), _dense(beta, "beta", x, (d,))
+    if out is not None:
+        _like(out, "out", x, x.shape)
+        ld_out = _row_shape(out, "out")[2]
+    with _place(x, stream):
+        if out is None:
+            out, ld_out = torch.empty(x.shape, dtype=x.dtype, device=x.device), d
+        mean = rstd = None
+        if save:
+            mean, rstd = torch.empty((2, M), dtype=torch.float32, device=x.device)
+        rc = load_library().ann_layer_norm(x.data_ptr(), ld, gp, bp, M, d, code, eps, out.data_ptr(), ld_out,
+                                           mean.data_ptr() if save else None, rstd.data_ptr() if save else None,
+                                           torch.cuda.current_stream().cuda_stream)
+    if rc:
+        _check(rc)
+    return (out, mean, rstd) if save else out
+
+
+def ann_layer_norm_backward_workspace_bytes(M: int, d: int, dtype: int) -> int:
+    n = load_library().ann_layer_norm_backward_workspace_bytes(M, d, dtype)
+    if n == 0:
+        raise AnnError(ANN_EINVAL, ann_last_error())
+    return int(n)
+
+
+def ann_layer_norm_backward(dout: torch.Tensor, x: torch.Tensor, gamma: Optional[torch.Tensor], mean: torch.Tensor,
+                            rstd: torch.Tensor, need_dx: bool = True, need_dparams: bool = True,
+                            workspace: Optional[torch.Tensor] = None, stream=None):
+    """(dx, dgamma, dbeta) of ann_layer_norm(x, gamma, beta, save=True); None for what is not needed."""
+    code = _row_code(x, "x")
+    M, d, ld = _row_shape(x, "x")
+    _like(dout, "dout", x, x.shape)
+    ld_dout = _row_shape(dout, "dout")[2]
+    gp = _dense(gamma, "gamma", x, (d,))
+    mp, rp = _dense(mean, "mean", x, (M,), torch.float32), _dense(rstd, "rstd", x, (M,), torch.float32)
+    lib = load_library()
+    with _place(x, stream):
+        dx = dparams = None
+        wp, wb = None, 0
+        if need_dx:
+            dx = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+        if need_dparams:
+            dparams = torch.empty((2, d), dtype=x.dtype, device=x.device)
+            workspace = _row_workspace(workspace, lib.ann_layer_norm_backward_workspace_bytes(M, d, code), x)
+            wp, wb = workspace.data_ptr(), workspace.numel()
+        dg = dparams.data_ptr() if need_dparams else None
+        rc = lib.ann_layer_norm_backward(dout.data_ptr(), ld_dout, x.data_ptr(), ld, gp, mp, rp, M, d, code,
+                                         dx.data_ptr() if need_dx else None, d, dg,
+                                         dg + d * x.element_size() if need_dparams else None, wp, wb,
+                                         torch.cuda.current_stream().cuda_stream)
+    if rc:
+        _check(rc)
+    return (dx, dparams[0], dparams[1]) if need_dparams else (dx, None, None)
+
+
+def ann_dropout(x: torch.Tensor, p: float, seed: int, draw: int = 0, residual: Optional[torch.Tensor] = None,
+                out: Optional[torch.Tensor] = None, draw_dev: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """residual + dropout of x (None = no residual), the choice a pure function of (seed, draw, element): the gradient
+    of x is ann_dropout(dout, p, seed, draw).  Contiguous tensors of one shape; `out` may be x or residual.  draw_dev
+    (one int64 on the device) is added to `draw` when the kernel runs: the replays of a recorded call draw anew."""
+    code = _row_code(x, "x")
+    if not x.is_contiguous():
+        raise ValueError("x must be contiguous")
+    rp = _dense(residual, "residual", x, x.shape)
+    op = _dense(out, "out", x, x.shape)
+    if draw_dev is not None and (draw_dev.numel() != 1 or draw_dev.device != x.device or
+                                 draw_dev.dtype not in (torch.int64, torch.uint64)):
+        raise ValueError(f"draw_dev must be one int64 on {x.device}")
+    with _place(x, stream):
+        if out is None:
+            out = torch.empty_like(x)
+            op = out.data_ptr()
+        rc = load_library().ann_dropout(x.data_ptr(), rp, op, x.numel(), code, p, seed, draw,
+                                        draw_dev.data_ptr() if draw_dev is not None else None,
+                                        torch.cuda.current_stream().cuda_stream)
+    if rc:
+        _check(rc)
+    return out
+
+
+def _ffn_shapes(x, w_in, w_out):
+    code = _row_code(x, "x")
+    M, D, ld = _row_shape(x, "x")
+    if w_in.dim() != 2 or w_out.dim() != 2 or w_in.shape[0] != 2 * w_out.shape[1]:
+        raise ValueError(f"w_in must be [2 * d_hidden][d_in] and w_out [d_out][d_hidden], got {tuple(w_in.shape)}, "
+                         f"{tuple(w_out.shape)}")
+    O, F = w_out.shape
+    return code, M, D, F, O, ld, _dense(w_in, "w_in", x, (2 * F, D)), _dense(w_out, "w_out", x, (O, F))
+
+
+def ann_gated_ffn_workspace_bytes(M: int, d_in: int, d_hidden: int, d_out: int, dtype: int) -> int:
+    n = load_library().ann_gated_ffn_workspace_bytes(M, d_in, d_hidden, d_out, dtype)
+    if n == 0:
+        raise AnnError(ANN_EINVAL, ann_last_error())
+    return int(n)
+
+
+def ann_gated_ffn(x: torch.Tensor, w_in: torch.Tensor, w_out: torch.Tensor, b_in: Optional[torch.Tensor] = None,
+                  b_out: Optional[torch.Tensor] = None, act: int = ANN_SILU, save: bool = False,
+                  out: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None, stream=None):
+    """(act(gate) * up) w_out^T + b_out with [gate | up] = x w_in^T + b_in: x [..., d_in], w_in [2 * d_hidden][d_in] (the gate's
+    rows first), w_out [d_out][d_hidden], all of one type.  With save=True (out, pre), pre [rows][2 * d_hidden] fp32, for
+    ann_gated_ffn_backward."""
+    code, M, D, F, O, ld, wip, wop = _ffn_shapes(x, w_in, w_out)
+    bip, bop = _dense(b_in, "b_in", x, (2 * F,)), _dense(b_out, "b_out", x, (O,))
+    shape, ld_out = x.shape[:-1] + (O,), O
+    if out is not None:
+        _like(out, "out", x, shape)
+        ld_out = _row_shape(out, "out")[2]
+    lib = load_library()
+    with _place(x, stream):
+        if out is None:
+            out = torch.empty(shape, dtype=x.dtype, device=x.device)
+        pre = torch.empty((M, 2 * F), dtype=torch.float32, device=x.device) if save else None
+        workspace = _row_workspace(workspace, lib.ann_gated_ffn_workspace_bytes(M, D, F, O, code), x)
+        rc = lib.ann_gated_ffn(x.data_ptr(), ld, wip, bip, wop, bop, M, D, F, O, act, code, out.data_ptr(), ld_out,
+                               pre.data_ptr() if save else None, workspace.data_ptr(), workspace.numel(),
+                               torch.cuda.current_stream().cuda_stream)
+    if rc:
+        _check(rc)
+    return (out, pre) if save else out
+
+
+def ann_gated_ffn_backward_workspace_bytes(M: int, d_in: int, d_hidden: int, d_out: int, dtype: int) -> int:
+    n = load_library().ann_gated_ffn_backward_workspace_bytes(M, d_in, d_hidden, d_out, dtype)
+    if n == 0:
+        raise AnnError(ANN_EINVAL, ann_last_error())
+    return int(n)
+
+
+def ann_gated_ffn_backward(dout: torch.Tensor, x: torch.Tensor, pre: torch.Tensor, w_in: torch.Tensor,
+                           w_out: torch.Tensor, act: int = ANN_SILU, bias: bool = False, need_dx: bool = True,
+                           need_dw: bool = True, workspace: Optional[torch.Tensor] = None, stream=None):
+    """(dx, dw_in, dw_out, db_in, db_out) of ann_gated_ffn(..., save=True); None for what is not needed (the last two
+    are given with bias=True)."""
+    code, M, D, F, O, ld, wip, wop = _ffn_shapes(x, w_in, w_out)
+    _like(dout, "dout", x, x.shape[:-1] + (O,))
+    ld_dout = _row_shape(dout, "dout")[2]
+    pp = _dense(pre, "pre", x, (M, 2 * F), torch.float32)
+    lib = load_library()
+    with _place(x, stream):
+        new = lambda *shape: torch.empty(shape, dtype=x.dtype, device=x.device)  # noqa: E731
+        dx = torch.empty(x.shape, dtype=x.dtype, device=x.device) if need_dx else None
+        dw_in, dw_out = (new(2 * F, D), new(O, F)) if need_dw else (None, None)
+        db_in, db_out = (new(2 * F), new(O)) if bias else (None, None)
+        workspace = _row_workspace(workspace, lib.ann_gated_ffn_backward_workspace_bytes(M, D, F, O, code), x)
+        ptr = lambda t: None if t is None else t.data_ptr()  # noqa: E731
+        rc = lib.ann_gated_ffn_backward(dout.data_ptr(), ld_dout, x.data_ptr(), ld, pp, wip, wop, M, D, F, O, act, code,
+                                        ptr(dx), D, ptr(dw_in), ptr(db_in), ptr(dw_out), ptr(db_out),
+                                        workspace.data_ptr(), workspace.numel(), torch.cuda.current_stream().cuda_stream)
+    if rc:
+        _check(rc)
+    return dx, dw_in, dw_out, db_in, db_out
 
 
 def ann_search_stats(workspace: torch.Tensor, stream=None) -> Stats:

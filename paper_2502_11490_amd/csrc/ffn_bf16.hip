@@ -1,0 +1,6 @@
+// The bf16 products of the gated feed-forward block.
+#include "ffn_mfma16.h"
+
+namespace gmpgr {
+template int launch_ffn16<ANN_BF16>(const FfnProduct &, hipStream_t);
+}

@@ -1,0 +1,67 @@
+// Element types and 16-byte accesses shared by the operators on rows of vectors (layer norm, dropout, the gated
+// feed-forward block).
+#pragma once
+
+#include "common.h"
+
+namespace gmpgr {
+
+template <int KIND> struct ElemOf;
+template <> struct ElemOf<ANN_F32> { using type = float; };
+template <> struct ElemOf<ANN_BF16> { using type = __bf16; };
+template <> struct ElemOf<ANN_F16> { using type = _Float16; };
+
+// 16 bytes of elements.  The type promises the element's own alignment only: gfx950 serves a 16-byte access at any
+// such address, so rows of odd widths and sliced tensors need no code of their own.
+template <typename T> constexpr int VEC = 16 / sizeof(T);
+template <typename T> struct __attribute__((packed, aligned(sizeof(T)))) Pack16 {
+    typedef T type __attribute__((ext_vector_type(16 / sizeof(T))));
+    type v;
+};
+
+template <typename T> __device__ __forceinline__ typename Pack16<T>::type load16(const T *p) {
+    return reinterpret_cast<const Pack16<T> *>(p)->v;
+}
+template <typename T> __device__ __forceinline__ void store16(T *p, typename Pack16<T>::type v) {
+    reinterpret_cast<Pack16<T> *>(p)->v = v;
+}
+
+// The VEC<T> elements from p on, the first `left` of them only (zeros behind).
+template <typename T> __device__ __forceinline__ void load_floats(const T *p, int left, float *out) {
+    if (left >= VEC<T>) {
+        const typename Pack16<T>::type v = load16(p);
+#pragma unroll
+        for (int i = 0; i < VEC<T>; ++i) out[i] = (float)v[i];
+    } else {
+#pragma unroll
+        for (int i = 0; i < VEC<T>; ++i) out[i] = i < left ? (float)p[i] : 0.f;
+    }
+}
+template <typename T> __device__ __forceinline__ void store_floats(T *p, int left, const float *in) {
+    if (left >= VEC<T>) {
+        typename Pack16<T>::type v;
+#pragma unroll
+        for (int i = 0; i < VEC<T>; ++i) v[i] = (T)in[i];
+        store16(p, v);
+    } else {
+#pragma unroll
+        for (int i = 0; i < VEC<T>; ++i)
+            if (i < left) p[i] = (T)in[i];
+    }
+}
+
+inline bool row_dtype(int32_t dtype) { return dtype == ANN_F32 || dtype == ANN_BF16 || dtype == ANN_F16; }
+inline size_t elem_bytes(int32_t dtype) { return dtype == ANN_F32 ? 4 : 2; }
+
+// rows.hip: out[c] = sum over P of part[p][c], in the order of p, rounded to KIND once; part [P][n] fp32
+int launch_sum_parts(const float *part, int64_t P, int64_t n, void *out, int dtype, hipStream_t stream);
+// rows.hip: the same for part [P][2][n] and two results, either of which may be null
+int launch_sum_two(const float *part, int64_t P, int64_t n, void *first, void *second, int dtype, hipStream_t stream);
+// rows.hip: n elements of zeros
+int launch_zero(void *out, int64_t n, int dtype, hipStream_t stream);
+// rows.hip: column sums of a [M][n] array of `dtype` (row stride ld), deterministic; part: column_sum_parts(M, n) * n floats
+int64_t column_sum_parts(int64_t M, int64_t n);
+int launch_column_sum(const void *in, int64_t M, int64_t n, int64_t ld, int in_dtype, void *out, int dtype, float *part,
+                      hipStream_t stream);
+
+}  // namespace gmpgr
