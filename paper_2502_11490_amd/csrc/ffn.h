@@ -16,21 +16,20 @@ enum FfnEpi {
 struct FfnArgs {
     const void *A, *B;
     int64_t lda, ldb;
-    int32_t M, N, K;      // FFN_GATE: N = d_hidden, B has 2 N rows
+    int32_t M, N, K;      // FFN_GATE: N = d_hidden, B has rows 0 .. N - 1 for the gate, up .. up + N - 1 for up
+    int32_t up;           // FFN_GRAD: C has the gate's columns from 0 and up's from `up` on
     void *C;
     int64_t ldc;
     const void *bias;     // [N], FFN_GATE: [2 N]; null = none
     float *pre;           // [M][2 N]: FFN_GATE writes it (null = not), FFN_GRAD reads it
-    void *h;              // [M][N], FFN_GRAD writes it (null = not)
+    void *h;              // [M][ldh], FFN_GRAD writes it (null = not)
+    int64_t ldh;
+    bool pad;             // C's rows are padded to 8 columns for the next product: zeros go behind the last one
     int32_t act;
     // sums over slices of k: slice s writes part[s][M][N or 2 N] in place of the epilogue
     float *part;
     int32_t splits, k_slice;
     int32_t tiles_m, tiles_n;
-};
-
-struct ActValue {
-    float value, slope;
 };
 
 // The activation and its derivative.  exp() in fp32 rows, the hardware's base-2 exponential in the 16-bit ones (2^-22
@@ -41,92 +40,131 @@ template <int KIND> __device__ __forceinline__ float ffn_exp(float z) {
 template <int KIND> __device__ __forceinline__ float ffn_sigmoid(float z) {
     return KIND == ANN_F32 ? 1.0f / (1.0f + expf(-z)) : sigmoid_hw(z);
 }
-template <int KIND> __device__ __forceinline__ ActValue ffn_act(int act, float z) {
-    if (act == ANN_RELU) return {z > 0.f ? z : (z <= 0.f ? 0.f : z), z > 0.f ? 1.f : 0.f};  // NaN stays NaN
-    if (act == ANN_GELU) {
-        const float cdf = 0.5f * (1.0f + erff(z * 0.70710678118654752f));
-        return {z * cdf, cdf + z * (0.39894228040143268f * ffn_exp<KIND>(-0.5f * z * z))};
-    }
-    const float sig = ffn_sigmoid<KIND>(z);
-    if (act == ANN_SILU) return {z * sig, sig * (1.0f + z * (1.0f - sig))};
-    return {sig, sig * (1.0f - sig)};
-}
-
-// Four consecutive elements, the first `left` of them.
-template <typename T> struct __attribute__((packed, aligned(sizeof(T)))) Pack4 {
-    typedef T type __attribute__((ext_vector_type(4)));
-    type v;
-};
-template <typename T> __device__ __forceinline__ void store4(T *p, int left, const float *v) {
-    if (left >= 4) {
-        typename Pack4<T>::type o = {(T)v[0], (T)v[1], (T)v[2], (T)v[3]};
-        reinterpret_cast<Pack4<T> *>(p)->v = o;
+// W of them; the choice is the same for the whole call, so it is taken once.
+template <int KIND, int W, bool SLOPE>
+__device__ __forceinline__ void ffn_act_each(int act, const float *z, float *value, float *slope) {
+    if (act == ANN_SILU || act == ANN_SIGMOID) {
+        const bool silu = act == ANN_SILU;
+#pragma unroll
+        for (int i = 0; i < W; ++i) {
+            const float sig = ffn_sigmoid<KIND>(z[i]), t = sig * (1.0f - sig);
+            value[i] = silu ? z[i] * sig : sig;
+            if (SLOPE) slope[i] = silu ? sig + z[i] * t : t;
+        }
+    } else if (act == ANN_GELU) {
+#pragma unroll
+        for (int i = 0; i < W; ++i) {
+            const float cdf = 0.5f * (1.0f + erff(z[i] * 0.70710678118654752f));
+            value[i] = z[i] * cdf;
+            if (SLOPE) slope[i] = cdf + z[i] * (0.39894228040143268f * ffn_exp<KIND>(-0.5f * z[i] * z[i]));
+        }
     } else {
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
+        for (int i = 0; i < W; ++i) {
+            value[i] = z[i] <= 0.f ? 0.f : z[i];  // NaN stays NaN
+            if (SLOPE) slope[i] = z[i] > 0.f ? 1.f : 0.f;
+        }
+    }
+}
+
+// W consecutive elements (8 to 32 bytes), the first `left` of them.
+template <typename T, int W> struct __attribute__((packed, aligned(sizeof(T)))) PackOf {
+    typedef T type __attribute__((ext_vector_type(W)));
+    type v;
+};
+template <int W, typename T> __device__ __forceinline__ void load_cols(const T *p, int left, float *v) {
+    constexpr int P = W * sizeof(T) > 16 ? 16 / sizeof(T) : W;  // elements of an access
+    if (left >= W) {
+#pragma unroll
+        for (int i = 0; i < W; i += P) {
+            const typename PackOf<T, P>::type t = reinterpret_cast<const PackOf<T, P> *>(p + i)->v;
+#pragma unroll
+            for (int j = 0; j < P; ++j) v[i + j] = (float)t[j];
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < W; ++i) v[i] = i < left ? (float)p[i] : 0.f;
+    }
+}
+template <int W, typename T> __device__ __forceinline__ void store_cols(T *p, int left, const float *v) {
+    constexpr int P = W * sizeof(T) > 16 ? 16 / sizeof(T) : W;
+    if (left >= W) {
+#pragma unroll
+        for (int i = 0; i < W; i += P) {
+            typename PackOf<T, P>::type t;
+#pragma unroll
+            for (int j = 0; j < P; ++j) t[j] = (T)v[i + j];
+            reinterpret_cast<PackOf<T, P> *>(p + i)->v = t;
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < W; ++i)
             if (i < left) p[i] = (T)v[i];
     }
 }
-template <typename T> __device__ __forceinline__ void load4(const T *p, int left, float *v) {
-    if (left >= 4) {
-        const typename Pack4<T>::type t = reinterpret_cast<const Pack4<T> *>(p)->v;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) v[i] = (float)t[i];
-    } else {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) v[i] = i < left ? (float)p[i] : 0.f;
+
+// What an epilogue reads of row m for W columns from n on; fetched ahead of the sums where that hides its way.
+template <int W> struct FfnRow {
+    float gate[W], up[W];
+};
+template <int W, int EPI> __device__ __forceinline__ void ffn_row(const FfnArgs &p, int64_t m, int n, FfnRow<W> &r) {
+    if (EPI == FFN_GRAD) {
+        const float *q = p.pre + m * 2 * p.N + n;
+        load_cols<W>(q, p.N - n, r.gate);
+        load_cols<W>(q + p.N, p.N - n, r.up);
     }
 }
 
-// Four consecutive columns n .. n + 3 of row m (the caller has m < M, n < N); `up` for FFN_GATE only.
-template <int KIND, int EPI>
-__device__ __forceinline__ void ffn_epilogue(const FfnArgs &p, int64_t m, int n, const float *sum, const float *up) {
+// W consecutive columns from n on of row m (the caller has m < M, n < N); `up` for FFN_GATE only.
+template <int KIND, int EPI, int W>
+__device__ __forceinline__ void ffn_epilogue(const FfnArgs &p, int64_t m, int n, const float *sum, const float *up,
+                                             const FfnRow<W> &r) {
     using T = typename ElemOf<KIND>::type;
     const int left = p.N - n;
     T *C = (T *)p.C + m * p.ldc + n;
-    float v[4], w[4];
+    float v[W], w[W];
     if (EPI == FFN_STORE) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) v[i] = sum[i];
+        for (int i = 0; i < W; ++i) v[i] = sum[i];
         if (p.bias) {
-            load4((const T *)p.bias + n, left, w);
+            load_cols<W>((const T *)p.bias + n, left, w);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) v[i] += w[i];
+            for (int i = 0; i < W; ++i) v[i] += w[i];
         }
-        store4(C, left, v);
+        store_cols<W>(C, left, v);
     } else if (EPI == FFN_GATE) {
-        float g[4], u[4];
+        float g[W], u[W];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) g[i] = sum[i], u[i] = up[i];
+        for (int i = 0; i < W; ++i) g[i] = sum[i], u[i] = up[i];
         if (p.bias) {
-            load4((const T *)p.bias + n, left, v);
-            load4((const T *)p.bias + p.N + n, left, w);
+            load_cols<W>((const T *)p.bias + n, left, v);
+            load_cols<W>((const T *)p.bias + p.N + n, left, w);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) g[i] += v[i], u[i] += w[i];
+            for (int i = 0; i < W; ++i) g[i] += v[i], u[i] += w[i];
         }
         if (p.pre) {
             float *q = p.pre + m * 2 * p.N + n;
-            store4(q, left, g);
-            store4(q + p.N, left, u);
+            store_cols<W>(q, left, g);
+            store_cols<W>(q + p.N, left, u);
         }
+        ffn_act_each<KIND, W, false>(p.act, g, v, nullptr);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) v[i] = ffn_act<KIND>(p.act, g[i]).value * u[i];
-        store4(C, left, v);
+        for (int i = 0; i < W; ++i) v[i] = i < left ? v[i] * u[i] : 0.f;
+        store_cols<W>(C, p.pad ? W : left, v);
     } else {
-        float g[4], u[4], h[4];
-        const float *q = p.pre + m * 2 * p.N + n;
-        load4(q, left, g);
-        load4(q + p.N, left, u);
+        float a[W], slope[W];
+        ffn_act_each<KIND, W, true>(p.act, r.gate, a, slope);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const ActValue a = ffn_act<KIND>(p.act, g[i]);
-            h[i] = a.value * u[i];
-            v[i] = sum[i] * u[i] * a.slope;
-            w[i] = sum[i] * a.value;
+        for (int i = 0; i < W; ++i) {
+            v[i] = sum[i] * r.up[i] * slope[i];
+            w[i] = sum[i] * a[i];
+            a[i] *= r.up[i];
         }
-        store4(C, left, v);
-        store4(C + p.N, left, w);
-        if (p.h) store4((T *)p.h + m * p.N + n, left, h);
+        store_cols<W>(C, left, v);
+        store_cols<W>(C + p.up, left, w);
+        if (p.pad && left < W)
+            for (int64_t i = p.up + p.N; i < p.ldc; ++i) ((T *)p.C + m * p.ldc)[i] = (T)0.f;
+        if (p.h) store_cols<W>((T *)p.h + m * p.ldh + n, left, a);
     }
 }
 
@@ -150,17 +188,29 @@ __device__ __forceinline__ FfnTile ffn_tile(const FfnArgs &p) {
     return t;
 }
 
-// One product; layouts: a_rows / b_rows = the operand's k are contiguous.  part: ffn_part_floats() floats.
+// One product: a_rows / b_rows = the operand's k are contiguous.
 struct FfnProduct {
     FfnArgs args;
     int kind, epi;
     bool a_rows, b_rows;
 };
-int ffn_splits(int kind, int64_t M, int64_t N, int64_t K, int epi);
-size_t ffn_part_floats(int kind, int64_t M, int64_t N, int64_t K, int epi);
+// How it is cut: tiles of tile x tile (FFN_GATE: half as many columns of C), k in `splits` slices.
+struct FfnCut {
+    int tile, splits;
+};
+FfnCut ffn_cut(int kind, int64_t M, int64_t N, int64_t K, int epi);
+size_t ffn_part_floats(int kind, int64_t M, int64_t N, int64_t K, int epi);  // what launch_ffn_product needs as `part`
 int launch_ffn_product(const FfnProduct &p, float *part, hipStream_t stream);
 
-template <int KIND> int launch_ffn16(const FfnProduct &p, hipStream_t stream);  // ffn_bf16.hip, ffn_f16.hip
-int launch_ffn32(const FfnProduct &p, hipStream_t stream);                      // ffn_f32.hip
+template <int KIND> int launch_ffn16(const FfnProduct &p, int tile, hipStream_t stream);  // ffn_bf16.hip, ffn_f16.hip
+int launch_ffn32(const FfnProduct &p, hipStream_t stream);                                // ffn_f32.hip
+
+// 16-bit operands as launch_ffn16 takes them: 16-byte aligned rows, the contiguous extent a multiple of 8, and 256 rows
+// within 2^30 bytes.
+inline bool ffn_direct(const void *p, int64_t ld, int64_t width) {
+    return (uintptr_t)p % 16 == 0 && ld % 8 == 0 && width % 8 == 0 && ld <= (int64_t)1 << 21;
+}
+// rows.hip: out [rows][ld_out] = in [rows][width], zeros in the columns behind; 16-bit elements
+int launch_pad_rows(const void *in, int64_t ld_in, int64_t rows, int64_t width, void *out, int64_t ld_out, hipStream_t stream);
 
 }  // namespace gmpgr

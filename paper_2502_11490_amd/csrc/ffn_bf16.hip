@@ -2,5 +2,5 @@
 #include "ffn_mfma16.h"
 
 namespace gmpgr {
-template int launch_ffn16<ANN_BF16>(const FfnProduct &, hipStream_t);
+template int launch_ffn16<ANN_BF16>(const FfnProduct &, int, hipStream_t);
 }

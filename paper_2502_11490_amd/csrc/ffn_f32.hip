@@ -36,7 +36,7 @@ template <bool KROWS, bool GATE> struct Operand32 {
             const int r = KROWS ? c >> 2 : (c & 31) * 4, k = k0 + (KROWS ? (c & 3) * 4 : c >> 5);
             const float *p = KROWS ? base + source_row(r) * ld + k : base + k * ld + r;
             float v[4];
-            load4(p, KROWS ? K - k : k < K ? rows - r : 0, v);
+            load_cols<4>(p, KROWS ? K - k : k < K ? rows - r : 0, v);
 #pragma unroll
             for (int e = 0; e < 4; ++e) regs[i][e] = v[e];
         }
@@ -67,7 +67,7 @@ template <bool A_ROWS, bool B_ROWS, int EPI> __global__ void __launch_bounds__(2
     Operand32<A_ROWS, false> a;
     Operand32<B_ROWS, GATE> b;
     a.init(p.A, p.lda, m0, p.M, 0);
-    b.init(p.B, p.ldb, n0, p.N, p.N);
+    b.init(p.B, p.ldb, n0, p.N, p.up);
     f32x16 acc[2][2];
 #pragma unroll
     for (int i = 0; i < 2; ++i)
@@ -125,10 +125,12 @@ template <bool A_ROWS, bool B_ROWS, int EPI> __global__ void __launch_bounds__(2
                 if (p.part) {
                     const int64_t width = GATE ? 2 * (int64_t)p.N : p.N;
                     float *o = p.part + ((int64_t)t.split * p.M + m) * width + n;
-                    store4(o, p.N - n, s);
-                    if (GATE) store4(o + p.N, p.N - n, u);
+                    store_cols<4>(o, p.N - n, s);
+                    if (GATE) store_cols<4>(o + p.N, p.N - n, u);
                 } else {
-                    ffn_epilogue<ANN_F32, EPI>(p, m, n, s, u);
+                    FfnRow<4> r;
+                    ffn_row<4, EPI>(p, m, n, r);
+                    ffn_epilogue<ANN_F32, EPI, 4>(p, m, n, s, u, r);
                 }
             }
     }

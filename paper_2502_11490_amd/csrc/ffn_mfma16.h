@@ -1,13 +1,17 @@
 // Products of the gated feed-forward block in the 16-bit types, on the matrix cores.
 //
-// A workgroup forms a BM x BN tile of C; its WM x WN waves each a part of (BM / WM) x (BN / WN) out of 16 x 16 x 32
-// matrix instructions.  64 of the k at a time lie in LDS, in two buffers: the next ones are on their way while the
-// present ones are multiplied.  An operand whose k are contiguous lies as [row][64 k], 128 bytes a row in 8 pieces
-// of 16, piece c at place c ^ (row & 7), and is read a piece a lane; one whose rows are contiguous lies as [64 k][rows],
-// and is read by the transposing LDS read (16 lanes fetch 4 k of 16 rows and get 4 k of a row each), its pieces at
-// c ^ 2 ((k & 3) | (k >> 3 & 1) << 2), which puts the eight k that half a wave reads at a time on eight different sets of banks.
-// FAST: global memory is loaded straight into LDS (16 bytes a lane, addresses in lane order, so the
-// permutation is in what a lane loads); it needs 16-byte aligned rows.  Otherwise through registers, any alignment.
+// A workgroup of 4 waves forms a BM x BN tile of C, a wave a quarter of it out of 16 x 16 x 32 matrix instructions.  64
+// of the k at a time lie in LDS, in two buffers.  A step goes in two halves of 32 k: while the matrix cores work on
+// one half's operands the next half's are read from LDS into a second set of registers, and half way through a
+// step, when every wave has read the last of the present buffer and the next one is there, one barrier lets the loads of
+// the step after next go out into it.  They have a whole step to arrive.
+//   An operand whose k are contiguous lies as [row][64 k], 128 bytes a row in 8 pieces of 16, piece c at place
+// c ^ (row & 7), and is read a piece a lane; one whose rows are contiguous lies as [64 k][rows], and is read by the
+// transposing LDS read (16 lanes fetch 4 k of 16 rows and get 4 k of a row each), its pieces at
+// c ^ 2 ((k & 3) | (k >> 3 & 1) << 2), which puts the eight k that half a wave reads at a time on eight different sets of
+// banks.  Global memory is loaded straight into LDS, 16 bytes a lane with addresses in lane order, so the permutation
+// is in what a lane loads; operands have 16-byte aligned rows and a contiguous extent that is a multiple of 8 (the
+// host packs those that do not).
 #pragma once
 
 #include "ffn.h"
@@ -18,104 +22,95 @@ typedef __attribute__((address_space(3))) void *LdsPtr;
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef short s16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef int i32x4 __attribute__((ext_vector_type(4)));
 
 template <int KIND> struct Frag16;
+// The sums stay where they are: the instruction as a statement whose sum is one accumulation register group in place.  (As a
+// builtin, with all 256 accumulation registers taken, the compiler moves the groups about: 140 copies a step.  The
+// statement is opaque to the compiler's wait states: its operands come straight from LDS reads, never from a vector
+// instruction, and the loop ends with the wait states of its last sums.)
 template <> struct Frag16<ANN_BF16> {
     typedef __bf16 type __attribute__((ext_vector_type(8)));
-    static __device__ __forceinline__ f32x4 mfma(type a, type b, f32x4 c) {
-        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+    static __device__ __forceinline__ void mfma(type a, type b, f32x4 &c) {
+        asm volatile("v_mfma_f32_16x16x32_bf16 %0, %1, %2, %0" : "+a"(c) : "v"(a), "v"(b));
     }
 };
 template <> struct Frag16<ANN_F16> {
     typedef _Float16 type __attribute__((ext_vector_type(8)));
-    static __device__ __forceinline__ f32x4 mfma(type a, type b, f32x4 c) {
-        return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
+    static __device__ __forceinline__ void mfma(type a, type b, f32x4 &c) {
+        asm volatile("v_mfma_f32_16x16x32_f16 %0, %1, %2, %0" : "+a"(c) : "v"(a), "v"(b));
     }
 };
 
 constexpr int FFN_BK = 64;
 constexpr uint32_t FFN_NOWHERE = 0x80000000u;  // an offset outside every buffer: such a load gives zeros
 
-// One operand's tile of ROWS rows by 64 k, loaded by THREADS threads.
-template <int KIND, bool KROWS, bool GATE, bool FAST, int ROWS, int THREADS>
-struct Operand16 {
+// One operand's tile of ROWS rows by 64 k, loaded by 256 threads.
+template <int KIND, bool KROWS, bool GATE, int ROWS> struct Operand16 {
     using T = typename ElemOf<KIND>::type;
-    static constexpr int PASSES = ROWS * 8 / THREADS;
+    using Frag = typename Frag16<KIND>::type;
+    static constexpr int PASSES = ROWS * 8 / 256;
     static constexpr int BYTES = ROWS * FFN_BK * 2;
     static constexpr int ACROSS = ROWS / 8;  // pieces of a line of [64 k][rows]
 
     const T *base;   // the tile's first row at k = 0
     int64_t ld;
-    int32_t rows;    // rows of the operand from the tile's first on; GATE: of one half
-    int32_t up;      // GATE: rows from a gate row to its up row
-    uint32_t offset[FAST ? PASSES : 1];
+    int32_t piece_k;             // KROWS: the k of this thread's pieces (of all passes)
+    uint32_t offset[PASSES];     // bytes from the tile's first row at the step's first k
 
-    // Piece c of the tile: which row (or first row) and k of the tile it holds.
-    static __device__ __forceinline__ int piece_row(int c) {
-        return KROWS ? c >> 3 : ((c & (ACROSS - 1)) ^ swizzle(c / ACROSS)) * 8;
-    }
-    static __device__ __forceinline__ int piece_k(int c) { return KROWS ? ((c & 7) ^ ((c >> 3) & 7)) * 8 : c / ACROSS; }
     static __device__ __forceinline__ int swizzle(int k) { return 2 * ((k & 3) | ((k >> 3) & 1) << 2); }
-    // GATE: rows of the tile go 16 of the gate, the same 16 of up, and so on
-    __device__ __forceinline__ int64_t source_row(int r) const {
-        if (!GATE) return r < rows ? r : rows - 1;
-        const int f = (r >> 5) * 16 + (r & 15);
-        return (int64_t)(f < rows ? f : rows - 1) + ((r >> 4) & 1 ? up : 0);
-    }
 
-    __device__ __forceinline__ void init(const void *p, int64_t ld_, int row0, int rows_, int up_) {
-        ld = ld_, rows = rows_ - row0, up = up_;
+    // row0: first row of the tile, rows: of the operand (GATE: of one half, up: rows from a gate row to its up row).
+    // GATE: rows of the tile go 16 of the gate, the same 16 of up, and so on.  Rows behind the last one repeat it.
+    __device__ __forceinline__ void init(const void *p, int64_t ld_, int row0, int rows, int up) {
+        ld = ld_;
         base = (const T *)p + (KROWS ? row0 * ld : (int64_t)row0);
-        if (FAST)
-#pragma unroll
-            for (int i = 0; i < PASSES; ++i) {
-                const int c = i * THREADS + threadIdx.x, r = piece_row(c), k = piece_k(c);
-                offset[i] = KROWS ? (uint32_t)((source_row(r) * ld + k) * 2)
-                                  : r < rows ? (uint32_t)((k * ld + r) * 2) : FFN_NOWHERE;
-            }
-    }
-
-    // FAST: sends for the pieces from k0 on (those at k >= K: zeros)
-    __device__ __forceinline__ void fetch(char *lds, int k0, int K) const {
-        const T *from = KROWS ? base + k0 : base + k0 * ld;
-        __amdgpu_buffer_rsrc_t rsrc = __builtin_amdgcn_make_buffer_rsrc((void *)from, 0, 0x7fffffff, 0x00020000);
-        const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        // a wave's pieces of a pass are all of the gate (the first two waves) or all of up
+        if (GATE) base += (int64_t)(__builtin_amdgcn_readfirstlane(threadIdx.x >> 7) * up) * ld;
+        piece_k = ((threadIdx.x & 7) ^ ((threadIdx.x >> 3) & 7)) * 8;
+        const int last = rows - row0 - 1;
 #pragma unroll
         for (int i = 0; i < PASSES; ++i) {
-            const uint32_t o = k0 + piece_k(i * THREADS + threadIdx.x) < K ? offset[i] : FFN_NOWHERE;
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (LdsPtr)(lds + (i * THREADS + wave * 64) * 16), 16, o, 0, 0, 0);
-        }
-    }
-
-    // otherwise: into registers, and from them into LDS
-    __device__ __forceinline__ void load(s16x8 *regs, int k0, int K) const {
-#pragma unroll
-        for (int i = 0; i < PASSES; ++i) {
-            const int c = i * THREADS + threadIdx.x, r = piece_row(c), k = k0 + piece_k(c);
-            const T *p = KROWS ? base + source_row(r) * ld + k : base + k * ld + r;
-            const int left = KROWS ? K - k : k < K ? rows - r : 0;
-            s16x8 v = {0, 0, 0, 0, 0, 0, 0, 0};
-            if (left >= 8) {
-                v = __builtin_bit_cast(s16x8, load16(p));
+            const int c = i * 256 + threadIdx.x;
+            if (KROWS) {
+                const int r = c >> 3, f = GATE ? (r >> 5) * 16 + (r & 15) : r;
+                offset[i] = (uint32_t)(((int64_t)(f < last ? f : last) * ld + piece_k) * 2);
             } else {
-#pragma unroll
-                for (int j = 0; j < 8; ++j)
-                    if (j < left) v[j] = __builtin_bit_cast(short, p[j]);
+                const int k = c / ACROSS, r = ((c & (ACROSS - 1)) ^ swizzle(k)) * 8;
+                offset[i] = r <= last ? (uint32_t)((k * ld + r) * 2) : FFN_NOWHERE;
             }
-            regs[i] = v;
         }
     }
-    static __device__ __forceinline__ void put(char *lds, const s16x8 *regs) {
+
+    // The buffer of the step at k0: its pieces, and for k >= K nothing but zeros (KROWS: see past()).
+    __device__ __forceinline__ i32x4 buffer(int k0, int K) const {
+        const uintptr_t from = (uintptr_t)(KROWS ? base + k0 : base + k0 * ld);
+        const int64_t left = (int64_t)(K - k0) * ld * 2;
+        const int bytes = KROWS || left > 0x7fffffff ? 0x7fffffff : left > 0 ? (int)left : 0;
+        return i32x4{(int)(uint32_t)from, (int)(uint32_t)(from >> 32) & 0xffff, bytes, 0x00020000};
+    }
+    __device__ __forceinline__ uint32_t past(int k0, int K) const { return KROWS && k0 + piece_k >= K ? FFN_NOWHERE : 0u; }
+
+    // Sends for pass i of a step's pieces: 16 bytes a lane, straight into LDS.  A statement, because the compiler lets no
+    // transposing LDS read go ahead of such a load; the waits are in the loop.  (m0 is the compiler's only from one
+    // instruction to the next.)
+    __device__ __forceinline__ void fetch(uint32_t lds, int i, i32x4 from, uint32_t past) const {
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
+                     ::"s"(lds + i * 4096), "v"(KROWS ? offset[i] | past : offset[i]), "s"(from));
+    }
+    __device__ __forceinline__ void fetch_all(uint32_t lds, int k0, int K) const {
+        const i32x4 from = buffer(k0, K);
+        const uint32_t none = past(k0, K);
 #pragma unroll
-        for (int i = 0; i < PASSES; ++i) *(s16x8 *)(lds + (i * THREADS + threadIdx.x) * 16) = regs[i];
+        for (int i = 0; i < PASSES; ++i) fetch(lds, i, from, none);
     }
 
     // The operand of a matrix instruction: rows row0 .. row0 + 15 (a lane's: row0 + lane % 16), k 32 ks + 8 (lane / 16) + 0 .. 7
-    static __device__ __forceinline__ typename Frag16<KIND>::type frag(const char *lds, int row0, int ks) {
+    static __device__ __forceinline__ Frag frag(const char *lds, int row0, int ks) {
         const int lane = threadIdx.x & 63, kg = lane >> 4, l = lane & 15;
         if (KROWS) {
             const int r = row0 + l;
-            return *(const typename Frag16<KIND>::type *)(lds + r * 128 + (((ks * 4 + kg) ^ (r & 7)) << 4));
+            return *(const Frag *)(lds + r * 128 + (((ks * 4 + kg) ^ (r & 7)) << 4));
         }
         const int k = ks * 32 + kg * 8 + (l >> 2);
         const int place = ((row0 >> 3) + ((l >> 1) & 1)) ^ (2 * ((l >> 2) | (kg & 1) << 2));
@@ -124,29 +119,32 @@ struct Operand16 {
         const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Quad)p);
         const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Quad)(p + 4 * ROWS * 2));
         const s16x8 v = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
-        return __builtin_bit_cast(typename Frag16<KIND>::type, v);
+        return __builtin_bit_cast(Frag, v);
     }
 };
 
-template <int KIND, bool A_ROWS, bool B_ROWS, bool FAST, int EPI, int BM, int BN, int WM, int WN>
-__global__ void __launch_bounds__(WM *WN * 64) ffn_mfma16_kernel(FfnArgs p) {
-    constexpr int THREADS = WM * WN * 64, MT = BM / WM / 16, NT = BN / WN / 16;
+template <int KIND, bool A_ROWS, bool B_ROWS, int EPI, int BM, int BN>
+__global__ void __launch_bounds__(256, BM == 256 ? 1 : 2) ffn_mfma16_kernel(FfnArgs p) {
+#ifdef __HIP_DEVICE_COMPILE__  // the registers that the statements name mean nothing to the host
+    constexpr int MT = BM / 32, NT = BN / 32;  // 16 x 16 pieces of a wave
     constexpr bool GATE = EPI == FFN_GATE;
-    constexpr int COLS = GATE ? BN / 2 : BN;  // columns of C
-    using OpA = Operand16<KIND, A_ROWS, false, FAST, BM, THREADS>;
-    using OpB = Operand16<KIND, B_ROWS, GATE, FAST, BN, THREADS>;
+    constexpr int COLS = GATE ? BN / 2 : BN;   // columns of C
+    using OpA = Operand16<KIND, A_ROWS, false, BM>;
+    using OpB = Operand16<KIND, B_ROWS, GATE, BN>;
+    using Frag = typename Frag16<KIND>::type;
     constexpr int BUFFER = OpA::BYTES + OpB::BYTES;
+    constexpr int LOADS = OpA::PASSES + OpB::PASSES;
     extern __shared__ __attribute__((aligned(1024))) char lds[];
 
     const FfnTile t = ffn_tile(p);
     const int m0 = t.m * BM, n0 = t.n * COLS;
     const int k_first = t.split * p.k_slice, K = k_first + p.k_slice < p.K ? k_first + p.k_slice : p.K;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
-    const int wm = (wave / WN) * (BM / WM), wn = (wave % WN) * (BN / WN);
+    const int wm = (wave >> 1) * (BM / 2), wn = (wave & 1) * (BN / 2);
     OpA a;
     OpB b;
     a.init(p.A, p.lda, m0, p.M, 0);
-    b.init(p.B, p.ldb, n0, p.N, p.N);
+    b.init(p.B, p.ldb, n0, p.N, p.up);
 
     f32x4 acc[MT][NT];
 #pragma unroll
@@ -154,82 +152,120 @@ __global__ void __launch_bounds__(WM *WN * 64) ffn_mfma16_kernel(FfnArgs p) {
 #pragma unroll
         for (int j = 0; j < NT; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
 
-    s16x8 ra[FAST ? 1 : OpA::PASSES], rb[FAST ? 1 : OpB::PASSES];
-    if (FAST) {
-        a.fetch(lds, k_first, K);
-        b.fetch(lds + OpA::BYTES, k_first, K);
-    } else {
-        a.load(ra, k_first, K);
-        b.load(rb, k_first, K);
-        OpA::put(lds, ra);
-        OpB::put(lds + OpA::BYTES, rb);
-    }
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    __syncthreads();
-    int buffer = 0;
-    for (int k = k_first; k < K; k += FFN_BK) {
-        char *now = lds + buffer * BUFFER, *next = lds + (buffer ^ 1) * BUFFER;
-        const bool more = k + FFN_BK < K;
-        if (more) {
-            if (FAST) {
-                a.fetch(next, k + FFN_BK, K);
-                b.fetch(next + OpA::BYTES, k + FFN_BK, K);
-            } else {
-                a.load(ra, k + FFN_BK, K);
-                b.load(rb, k + FFN_BK, K);
-            }
-        }
+    // where this wave's pieces of a pass go
+    const uint32_t lds_at = (uint32_t)(uintptr_t)(LdsPtr)lds + wave * 1024;
+    a.fetch_all(lds_at, k_first, K);
+    b.fetch_all(lds_at + OpA::BYTES, k_first, K);
+    a.fetch_all(lds_at + BUFFER, k_first + FFN_BK, K);
+    b.fetch_all(lds_at + BUFFER + OpA::BYTES, k_first + FFN_BK, K);
+    asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"(LOADS) : "memory");
+    Frag fa[2][MT], fb[2][NT];
 #pragma unroll
-        for (int ks = 0; ks < 2; ++ks) {
-            typename Frag16<KIND>::type fa[MT], fb[NT];
+    for (int j = 0; j < NT; ++j) fb[0][j] = OpB::frag(lds + OpA::BYTES, wn + j * 16, 0);
 #pragma unroll
-            for (int j = 0; j < NT; ++j) fb[j] = OpB::frag(now + OpA::BYTES, wn + j * 16, ks);
-#pragma unroll
-            for (int i = 0; i < MT; ++i) fa[i] = OpA::frag(now, wm + i * 16, ks);
-#pragma unroll
-            for (int i = 0; i < MT; ++i)
-#pragma unroll
-                for (int j = 0; j < NT; ++j) acc[i][j] = Frag16<KIND>::mfma(fb[j], fa[i], acc[i][j]);
-        }
-        if (!FAST && more) {
-            OpA::put(next, ra);
-            OpB::put(next + OpA::BYTES, rb);
-        }
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-        __syncthreads();
-        buffer ^= 1;
-    }
+    for (int i = 0; i < MT; ++i) fa[0][i] = OpA::frag(lds, wm + i * 16, 0);
 
-    // A lane has columns 4 (lane / 16) .. + 3 of row lane % 16 of every 16 x 16 piece.
+    int buffer = 0;
+    for (int k = k_first; k < K; k += FFN_BK, buffer ^= 1) {
+        const char *now = lds + buffer * BUFFER, *next = lds + (buffer ^ 1) * BUFFER;
+        const uint32_t to = lds_at + buffer * BUFFER;
+        const i32x4 from_a = a.buffer(k + 2 * FFN_BK, K), from_b = b.buffer(k + 2 * FFN_BK, K);
+        const uint32_t past_a = a.past(k + 2 * FFN_BK, K), past_b = b.past(k + 2 * FFN_BK, K);
 #pragma unroll
-    for (int i = 0; i < MT; ++i) {
-        const int64_t m = m0 + wm + i * 16 + (lane & 15);
-        if (m >= p.M) continue;
+        for (int half = 0; half < 2; ++half) {
+            const char *from = half ? next : now;
+            if (half) asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+            __builtin_amdgcn_sched_barrier(0);
+            // the matrix instructions in order, and between them one after the other what the next half needs
 #pragma unroll
-        for (int j = 0; j < NT; j += GATE ? 2 : 1) {
-            const int n = n0 + (GATE ? (wn + j * 16) / 2 : wn + j * 16) + (lane >> 4) * 4;
-            if (n >= p.N) continue;
-            float s[4], u[4];
+            for (int x = 0; x < MT * NT; ++x) {
+                constexpr int READ_EACH = MT * NT / 2 / (MT + NT), LOAD_EACH = MT * NT / LOADS;
+                if (half && x % LOAD_EACH == 0) {
+                    const int y = x / LOAD_EACH;
+                    if (y < OpA::PASSES) a.fetch(to, y, from_a, past_a);
+                    else b.fetch(to + OpA::BYTES, y - OpA::PASSES, from_b, past_b);
+                }
+                if (x % READ_EACH == READ_EACH - 1) {
+                    const int y = x / READ_EACH;
+                    if (y < NT) fb[half ^ 1][y] = OpB::frag(from + OpA::BYTES, wn + y * 16, half ^ 1);
+                    else if (y < NT + MT) fa[half ^ 1][y - NT] = OpA::frag(from, wm + (y - NT) * 16, half ^ 1);
+                }
+                Frag16<KIND>::mfma(fb[half][x % NT], fa[half][x / NT], acc[x / NT][x % NT]);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        }
+        asm volatile("s_nop 15\n\ts_nop 3");  // the last sums are there before anything the compiler puts behind the loop
+    }
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // the loads past the end write to LDS
 #pragma unroll
-            for (int e = 0; e < 4; ++e) s[e] = acc[i][j][e], u[e] = GATE ? acc[i][j + (GATE ? 1 : 0)][e] : 0.f;
-            if (p.part) {
-                const int64_t width = GATE ? 2 * (int64_t)p.N : p.N;
-                float *q = p.part + ((int64_t)t.split * p.M + m) * width + n;
-                store4(q, p.N - n, s);
-                if (GATE) store4(q + p.N, p.N - n, u);
-            } else {
-                ffn_epilogue<KIND, EPI>(p, m, n, s, u);
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int j = 0; j < NT; ++j) asm volatile("" : "+a"(acc[i][j]));
+    __builtin_amdgcn_sched_barrier(0);
+
+    // The sums go through LDS, half of the wave's rows at a time and each wave in a part of its own, and from there 8 columns
+    // a lane, row after row, to the epilogue: the instruction leaves 4 columns of 16 rows in a lane, which would be
+    // pieces of 8 bytes of 16 lines a store.  Piece q (4 columns) of row r lies at q ^ (r & 15).
+    __syncthreads();
+    constexpr int WN = BN / 2, HALF = MT / 2 * 16;
+    constexpr int WIDE = GATE ? WN / 2 : WN, LANES = WIDE / 8, ROWS = 64 / LANES;  // columns of C, lanes a row, rows at a time
+    float *const mine = (float *)lds + wave * HALF * WN;
+    const int lane_row = lane / LANES, c = (lane % LANES) * 8;                     // c: first of the lane's columns
+    const int n = n0 + (GATE ? wn / 2 : wn) + c;
+    const int q0 = GATE ? (c >> 4) * 8 + (c & 15) / 4 : c / 4;                     // GATE: 16 columns of the gate, 16 of up, ...
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+#pragma unroll
+        for (int i = 0; i < MT / 2; ++i)
+#pragma unroll
+            for (int j = 0; j < NT; ++j)
+                *(f32x4 *)(mine + (i * 16 + (lane & 15)) * WN + ((j * 4 + (lane >> 4)) ^ (lane & 15)) * 4) =
+                    acc[half * (MT / 2) + i][j];
+        const int64_t m_first = m0 + wm + half * HALF;
+        constexpr int AHEAD = HALF / ROWS < 4 ? HALF / ROWS : 4;  // rows whose gate and up values are on their way together
+        for (int r0 = 0; r0 < HALF; r0 += ROWS * AHEAD) {
+            FfnRow<8> row[AHEAD];
+#pragma unroll
+            for (int x = 0; x < AHEAD; ++x) {
+                const int64_t m = m_first + r0 + x * ROWS + lane_row;
+                if (EPI == FFN_GRAD && !p.part && m < p.M && n < p.N) ffn_row<8, EPI>(p, m, n, row[x]);
+            }
+#pragma unroll
+            for (int x = 0; x < AHEAD; ++x) {
+                const int r = r0 + x * ROWS + lane_row;
+                const int64_t m = m_first + r;
+                if (m >= p.M || n >= p.N) continue;
+                float s[8], u[8];
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    const f32x4 v = *(const f32x4 *)(mine + r * WN + ((q0 + e) ^ (r & 15)) * 4);
+#pragma unroll
+                    for (int f = 0; f < 4; ++f) s[e * 4 + f] = v[f], u[e * 4 + f] = 0.f;
+                    if (GATE) {
+                        const f32x4 w = *(const f32x4 *)(mine + r * WN + ((q0 + 4 + e) ^ (r & 15)) * 4);
+#pragma unroll
+                        for (int f = 0; f < 4; ++f) u[e * 4 + f] = w[f];
+                    }
+                }
+                if (p.part) {
+                    const int64_t width = GATE ? 2 * (int64_t)p.N : p.N;
+                    float *o = p.part + ((int64_t)t.split * p.M + m) * width + n;
+                    store_cols<8>(o, p.N - n, s);
+                    if (GATE) store_cols<8>(o + p.N, p.N - n, u);
+                } else {
+                    ffn_epilogue<KIND, EPI, 8>(p, m, n, s, u, row[x]);
+                }
             }
         }
     }
+#endif
 }
 
-template <int KIND, bool A_ROWS, bool B_ROWS, bool FAST, int EPI, int BM, int BN, int WM, int WN>
-int launch_tile16(FfnArgs a, hipStream_t stream) {
+template <int KIND, bool A_ROWS, bool B_ROWS, int EPI, int BM, int BN> int launch_tile16(FfnArgs a, hipStream_t stream) {
     constexpr size_t LDS = 2 * (size_t)(BM + BN) * FFN_BK * 2;
     constexpr int COLS = EPI == FFN_GATE ? BN / 2 : BN;
     static std::atomic<uint32_t> done{0};
-    auto fn = ffn_mfma16_kernel<KIND, A_ROWS, B_ROWS, FAST, EPI, BM, BN, WM, WN>;
+    auto fn = ffn_mfma16_kernel<KIND, A_ROWS, B_ROWS, EPI, BM, BN>;
     int device = 0;
     ANN_HIP_TRY(hipGetDevice(&device));
     const int rc = raise_lds_limit((const void *)fn, LDS, device, done);
@@ -241,30 +277,23 @@ int launch_tile16(FfnArgs a, hipStream_t stream) {
         set_error("a product of %d x %d has too many tiles", a.M, a.N);
         return ANN_ENOTIMPL;
     }
-    hipLaunchKernelGGL(fn, dim3((unsigned)total), dim3(WM * WN * 64), LDS, stream, a);
+    hipLaunchKernelGGL(fn, dim3((unsigned)total), dim3(256), LDS, stream, a);
     ANN_HIP_TRY(hipGetLastError());
     return ANN_OK;
 }
 
-// Rows that 16-byte loads straight into LDS can take: 16-byte aligned, pieces that do not straddle an end, and offsets
-// inside a tile that fit 31 bits.
-inline bool direct_operand(const void *p, int64_t ld, bool k_rows, int64_t rows, int64_t K, int64_t up) {
-    return (uintptr_t)p % 16 == 0 && ld % 8 == 0 && (k_rows ? K : rows) % 8 == 0 && ((k_rows ? up : 0) + 256) * ld < ((int64_t)1 << 30);
+template <int KIND, bool A_ROWS, bool B_ROWS, int EPI>
+int launch_layout16(const FfnArgs &a, int tile, hipStream_t stream) {
+    return tile == 256 ? launch_tile16<KIND, A_ROWS, B_ROWS, EPI, 256, 256>(a, stream)
+                       : launch_tile16<KIND, A_ROWS, B_ROWS, EPI, 128, 128>(a, stream);
 }
 
-template <int KIND, bool A_ROWS, bool B_ROWS, int EPI> int launch_layout16(const FfnArgs &a, hipStream_t stream) {
-    const bool fast = direct_operand(a.A, a.lda, A_ROWS, a.M, a.K, 0) &&
-                      direct_operand(a.B, a.ldb, B_ROWS, a.N, a.K, EPI == FFN_GATE ? a.N : 0);
-    return fast ? launch_tile16<KIND, A_ROWS, B_ROWS, true, EPI, 128, 128, 2, 2>(a, stream)
-                : launch_tile16<KIND, A_ROWS, B_ROWS, false, EPI, 128, 128, 2, 2>(a, stream);
-}
-
-template <int KIND> int launch_ffn16(const FfnProduct &p, hipStream_t stream) {
-    if (p.epi == FFN_GATE) return launch_layout16<KIND, true, true, FFN_GATE>(p.args, stream);
-    if (p.epi == FFN_GRAD) return launch_layout16<KIND, true, false, FFN_GRAD>(p.args, stream);
-    if (p.a_rows && p.b_rows) return launch_layout16<KIND, true, true, FFN_STORE>(p.args, stream);
-    if (p.a_rows) return launch_layout16<KIND, true, false, FFN_STORE>(p.args, stream);
-    return launch_layout16<KIND, false, false, FFN_STORE>(p.args, stream);
+template <int KIND> int launch_ffn16(const FfnProduct &p, int tile, hipStream_t stream) {
+    if (p.epi == FFN_GATE) return launch_layout16<KIND, true, true, FFN_GATE>(p.args, tile, stream);
+    if (p.epi == FFN_GRAD) return launch_layout16<KIND, true, false, FFN_GRAD>(p.args, tile, stream);
+    if (p.a_rows && p.b_rows) return launch_layout16<KIND, true, true, FFN_STORE>(p.args, tile, stream);
+    if (p.a_rows) return launch_layout16<KIND, true, false, FFN_STORE>(p.args, tile, stream);
+    return launch_layout16<KIND, false, false, FFN_STORE>(p.args, tile, stream);
 }
 
 }  // namespace gmpgr

@@ -8,30 +8,34 @@
 
 namespace gmpgr {
 
-// Joins the slices of a product that was cut along k and applies its epilogue: four columns a thread.
+// Joins the slices of a product that was cut along k and applies its epilogue: 8 columns a thread.
 template <int KIND, int EPI> __global__ void __launch_bounds__(256) ffn_finish_kernel(FfnArgs p) {
-    const int64_t quads = (p.N + 3) / 4, total = quads * p.M, width = EPI == FFN_GATE ? 2 * (int64_t)p.N : p.N;
+    constexpr int W = 8;
+    const int64_t across = (p.N + W - 1) / W, total = across * p.M, width = EPI == FFN_GATE ? 2 * (int64_t)p.N : p.N;
     for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
-        const int64_t m = i / quads;
-        const int n = (int)(i - m * quads) * 4, left = p.N - n;
-        float s[4] = {0.f, 0.f, 0.f, 0.f}, u[4] = {0.f, 0.f, 0.f, 0.f}, v[4];
+        const int64_t m = i / across;
+        const int n = (int)(i - m * across) * W, left = p.N - n;
+        float s[W] = {}, u[W] = {}, v[W];
+        FfnRow<W> r;
+        ffn_row<W, EPI>(p, m, n, r);
+#pragma unroll 4
         for (int c = 0; c < p.splits; ++c) {
             const float *q = p.part + ((int64_t)c * p.M + m) * width + n;
-            load4(q, left, v);
+            load_cols<W>(q, left, v);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) s[e] += v[e];
+            for (int e = 0; e < W; ++e) s[e] += v[e];
             if (EPI == FFN_GATE) {
-                load4(q + p.N, left, v);
+                load_cols<W>(q + p.N, left, v);
 #pragma unroll
-                for (int e = 0; e < 4; ++e) u[e] += v[e];
+                for (int e = 0; e < W; ++e) u[e] += v[e];
             }
         }
-        ffn_epilogue<KIND, EPI>(p, m, n, s, u);
+        ffn_epilogue<KIND, EPI, W>(p, m, n, s, u, r);
     }
 }
 
 template <int KIND> static int launch_finish(const FfnArgs &a, int epi, hipStream_t stream) {
-    const int64_t groups = ((int64_t)((a.N + 3) / 4) * a.M + 255) / 256;
+    const int64_t groups = ((int64_t)((a.N + 7) / 8) * a.M + 255) / 256;
     auto fn = epi == FFN_GATE   ? ffn_finish_kernel<KIND, FFN_GATE>
               : epi == FFN_GRAD ? ffn_finish_kernel<KIND, FFN_GRAD>
                                 : ffn_finish_kernel<KIND, FFN_STORE>;
@@ -40,33 +44,41 @@ template <int KIND> static int launch_finish(const FfnArgs &a, int epi, hipStrea
     return ANN_OK;
 }
 
-// Slices of k: enough workgroups for two a compute unit where the tiles alone are not, each slice with 4 or more steps
-// of 64, and at most 16 (each costs a write and a read of the whole result in fp32).
-int ffn_splits(int kind, int64_t M, int64_t N, int64_t K, int epi) {
-    const int64_t cols = epi == FFN_GATE ? 64 : 128, tiles = ((M + 127) / 128) * ((N + cols - 1) / cols);
-    (void)kind;
-    int64_t s = 512 / (tiles < 1 ? 1 : tiles);
-    if (s > K / 256) s = K / 256;
-    if (s > 16) s = 16;
-    return s < 1 ? 1 : (int)s;
+// The cut that a simple account says is fastest: rounds of workgroups over 256 compute units (one of the 256 x 256 tiles a
+// unit, two of the others), each round as many steps of 64 k as a slice has, a round's start and end, and for slices the
+// writing and reading of the parts and one more launch.
+FfnCut ffn_cut(int kind, int64_t M, int64_t N, int64_t K, int epi) {
+    FfnCut best = {128, 1};
+    double least = 0.0;
+    for (int tile = 128; tile <= (kind == ANN_F32 ? 128 : 256); tile *= 2) {
+        const int64_t cols = epi == FFN_GATE ? tile / 2 : tile, tiles = ((M + tile - 1) / tile) * ((N + cols - 1) / cols);
+        const double step = kind == ANN_F32 ? 5.0 : tile == 256 ? 1.7 : 1.1, ends = tile == 256 ? 10.0 : 5.0;  // microseconds
+        for (int s = 1; s <= 16 && (s == 1 || s <= K / 256); s += s < 4 ? 1 : 2) {
+            const int64_t slots = tile == 256 ? 256 : 512, rounds = (tiles * s + slots - 1) / slots;
+            const double steps = (double)((K + 64 * s - 1) / (64 * s));
+            double t = (double)rounds * (steps * step + ends);
+            if (s > 1) t += 4.0 + 8.0 * s * (double)M * (double)N * (epi == FFN_GATE ? 2 : 1) / 4.0e6;
+            if (least == 0.0 || t < least) least = t, best = {tile, s};
+        }
+    }
+    return best;
 }
 
 size_t ffn_part_floats(int kind, int64_t M, int64_t N, int64_t K, int epi) {
-    const int s = ffn_splits(kind, M, N, K, epi);
+    const int s = ffn_cut(kind, M, N, K, epi).splits;
     return s > 1 ? (size_t)s * (size_t)M * (size_t)N * (epi == FFN_GATE ? 2 : 1) : 0;
 }
 
 int launch_ffn_product(const FfnProduct &product, float *part, hipStream_t stream) {
     FfnProduct p = product;
     FfnArgs &a = p.args;
-    const int s = ffn_splits(p.kind, a.M, a.N, a.K, p.epi);
-    a.k_slice = (int32_t)((((int64_t)a.K + s - 1) / s + 63) / 64 * 64);
-    if (s == 1) a.k_slice = a.K;
+    const FfnCut cut = ffn_cut(p.kind, a.M, a.N, a.K, p.epi);
+    a.k_slice = cut.splits == 1 ? a.K : (int32_t)((((int64_t)a.K + cut.splits - 1) / cut.splits + 63) / 64 * 64);
     a.splits = (int32_t)(((int64_t)a.K + a.k_slice - 1) / a.k_slice);
     a.part = a.splits > 1 ? part : nullptr;
     const int rc = p.kind == ANN_F32    ? launch_ffn32(p, stream)
-                   : p.kind == ANN_BF16 ? launch_ffn16<ANN_BF16>(p, stream)
-                                        : launch_ffn16<ANN_F16>(p, stream);
+                   : p.kind == ANN_BF16 ? launch_ffn16<ANN_BF16>(p, cut.tile, stream)
+                                        : launch_ffn16<ANN_F16>(p, cut.tile, stream);
     if (rc != ANN_OK || a.splits == 1) return rc;
     return p.kind == ANN_F32    ? launch_finish<ANN_F32>(a, p.epi, stream)
            : p.kind == ANN_BF16 ? launch_finish<ANN_BF16>(a, p.epi, stream)
@@ -81,36 +93,59 @@ struct Region {
         return at;
     }
 };
-struct ForwardPlan {
-    size_t h, part, total;
-};
-struct BackwardPlan {
-    size_t dpre, h, part, total;
+// Parts of a workspace.  x, w_in, w_out, dout: copies of operands whose rows the 16-bit kernels cannot load as they lie (an
+// odd width, stride or address); kept free for every call, because a workspace is sized before the addresses are known.
+struct FfnPlan {
+    size_t x, w_in, w_out, dout, dpre, h, part, total;
+    int64_t D8, F8, O8, ld_pre;  // row strides of the copies, of h and of dpre (fp32: as wide as the rows)
 };
 static size_t most(size_t a, size_t b) { return a > b ? a : b; }
 
-static ForwardPlan forward_plan(int64_t M, int64_t D, int64_t F, int64_t O, int dtype) {
+static FfnPlan ffn_plan(int64_t M, int64_t D, int64_t F, int64_t O, int dtype, bool gradient) {
     Region r;
-    ForwardPlan p;
-    p.h = r.take((size_t)M * F * elem_bytes(dtype));
-    p.part = r.take(sizeof(float) * most(ffn_part_floats(dtype, M, F, D, FFN_GATE), ffn_part_floats(dtype, M, O, F, FFN_STORE)));
-    p.total = r.total + 256;
-    return p;
-}
-static BackwardPlan backward_plan(int64_t M, int64_t D, int64_t F, int64_t O, int dtype) {
-    Region r;
-    BackwardPlan p;
-    p.dpre = r.take((size_t)M * 2 * F * elem_bytes(dtype));
-    p.h = r.take((size_t)M * F * elem_bytes(dtype));
-    size_t n = ffn_part_floats(dtype, M, F, O, FFN_GRAD);
-    n = most(n, ffn_part_floats(dtype, M, D, 2 * F, FFN_STORE));
-    n = most(n, ffn_part_floats(dtype, 2 * F, D, M, FFN_STORE));
-    n = most(n, ffn_part_floats(dtype, O, F, M, FFN_STORE));
-    n = most(n, (size_t)column_sum_parts(M, 2 * F) * 2 * F);
-    n = most(n, (size_t)column_sum_parts(M, O) * O);
+    FfnPlan p = {};
+    const size_t e = elem_bytes(dtype);
+    const bool pack = dtype != ANN_F32;
+    const int64_t to = pack ? 8 : 1;
+    p.D8 = (D + to - 1) / to * to, p.F8 = (F + to - 1) / to * to, p.O8 = (O + to - 1) / to * to;
+    p.ld_pre = (2 * F + to - 1) / to * to;
+    p.h = r.take((size_t)M * p.F8 * e);
+    if (pack) {
+        p.x = r.take((size_t)M * p.D8 * e);
+        p.w_in = r.take((size_t)2 * F * p.D8 * e);
+        p.w_out = r.take((size_t)O * p.F8 * e);
+    }
+    size_t n;
+    if (!gradient) {
+        n = most(ffn_part_floats(dtype, M, F, D, FFN_GATE), ffn_part_floats(dtype, M, O, F, FFN_STORE));
+    } else {
+        if (pack) p.dout = r.take((size_t)M * p.O8 * e);
+        p.dpre = r.take((size_t)M * p.ld_pre * e);
+        n = ffn_part_floats(dtype, M, F, O, FFN_GRAD);
+        n = most(n, ffn_part_floats(dtype, M, D, 2 * F, FFN_STORE));
+        n = most(n, ffn_part_floats(dtype, 2 * F, D, M, FFN_STORE));
+        n = most(n, ffn_part_floats(dtype, O, F, M, FFN_STORE));
+        n = most(n, (size_t)column_sum_parts(M, 2 * F) * 2 * F);
+        n = most(n, (size_t)column_sum_parts(M, O) * O);
+    }
     p.part = r.take(sizeof(float) * n);
     p.total = r.total + 256;
     return p;
+}
+
+// An operand as the product's kernels take it: itself, or its copy in the workspace.
+struct Rows {
+    const void *p;
+    int64_t ld;
+};
+static int ffn_rows(int dtype, const void *p, int64_t ld, int64_t rows, int64_t width, char *copy, int64_t ld_copy,
+                    hipStream_t stream, Rows *out) {
+    if (dtype == ANN_F32 || ffn_direct(p, ld, width)) {
+        *out = {p, ld};
+        return ANN_OK;
+    }
+    *out = {copy, ld_copy};
+    return launch_pad_rows(p, ld, rows, width, copy, ld_copy, stream);
 }
 
 static bool ffn_sizes(int64_t M, int32_t D, int32_t F, int32_t O, int32_t dtype) {
@@ -163,11 +198,11 @@ using namespace gmpgr;
 extern "C" {
 
 size_t ann_gated_ffn_workspace_bytes(int64_t M, int32_t d_in, int32_t d_hidden, int32_t d_out, int32_t dtype) {
-    return ffn_sizes(M, d_in, d_hidden, d_out, dtype) ? forward_plan(M, d_in, d_hidden, d_out, dtype).total : 0;
+    return ffn_sizes(M, d_in, d_hidden, d_out, dtype) ? ffn_plan(M, d_in, d_hidden, d_out, dtype, false).total : 0;
 }
 
 size_t ann_gated_ffn_backward_workspace_bytes(int64_t M, int32_t d_in, int32_t d_hidden, int32_t d_out, int32_t dtype) {
-    return ffn_sizes(M, d_in, d_hidden, d_out, dtype) ? backward_plan(M, d_in, d_hidden, d_out, dtype).total : 0;
+    return ffn_sizes(M, d_in, d_hidden, d_out, dtype) ? ffn_plan(M, d_in, d_hidden, d_out, dtype, true).total : 0;
 }
 
 int ann_gated_ffn(const void *x_dev, int64_t ld_x, const void *w_in_dev, const void *b_in_dev, const void *w_out_dev,
@@ -191,20 +226,26 @@ int ann_gated_ffn(const void *x_dev, int64_t ld_x, const void *w_in_dev, const v
         set_error("out_dev must not overlap x_dev");
         return rc;
     }
-    const ForwardPlan plan = forward_plan(M, d_in, d_hidden, d_out, dtype);
+    const FfnPlan plan = ffn_plan(M, d_in, d_hidden, d_out, dtype, false);
     if (!ffn_workspace(workspace_dev, workspace_bytes, plan.total, &rc)) return rc;
     char *ws = (char *)workspace_dev;
     hipStream_t s = (hipStream_t)stream;
+    Rows x, w_in, w_out;
+    rc = ffn_rows(dtype, x_dev, ld_x, M, d_in, ws + plan.x, plan.D8, s, &x);
+    if (rc == ANN_OK) rc = ffn_rows(dtype, w_in_dev, d_in, (int64_t)2 * d_hidden, d_in, ws + plan.w_in, plan.D8, s, &w_in);
+    if (rc == ANN_OK) rc = ffn_rows(dtype, w_out_dev, d_hidden, d_out, d_hidden, ws + plan.w_out, plan.F8, s, &w_out);
+    if (rc != ANN_OK) return rc;
     FfnProduct p = {};
     p.kind = dtype, p.epi = FFN_GATE, p.a_rows = true, p.b_rows = true;
-    p.args.A = x_dev, p.args.lda = ld_x, p.args.B = w_in_dev, p.args.ldb = d_in;
-    p.args.M = (int32_t)M, p.args.N = d_hidden, p.args.K = d_in;
-    p.args.C = ws + plan.h, p.args.ldc = d_hidden, p.args.bias = b_in_dev, p.args.pre = pre_dev, p.args.act = act;
+    p.args.A = x.p, p.args.lda = x.ld, p.args.B = w_in.p, p.args.ldb = w_in.ld;
+    p.args.M = (int32_t)M, p.args.N = d_hidden, p.args.K = d_in, p.args.up = d_hidden;
+    p.args.C = ws + plan.h, p.args.ldc = plan.F8, p.args.pad = dtype != ANN_F32;
+    p.args.bias = b_in_dev, p.args.pre = pre_dev, p.args.act = act;
     rc = launch_ffn_product(p, (float *)(ws + plan.part), s);
     if (rc != ANN_OK) return rc;
     FfnProduct q = {};
     q.kind = dtype, q.epi = FFN_STORE, q.a_rows = true, q.b_rows = true;
-    q.args.A = ws + plan.h, q.args.lda = d_hidden, q.args.B = w_out_dev, q.args.ldb = d_hidden;
+    q.args.A = ws + plan.h, q.args.lda = plan.F8, q.args.B = w_out.p, q.args.ldb = w_out.ld;
     q.args.M = (int32_t)M, q.args.N = d_out, q.args.K = d_hidden;
     q.args.C = out_dev, q.args.ldc = ld_out, q.args.bias = b_out_dev;
     return launch_ffn_product(q, (float *)(ws + plan.part), s);
@@ -244,47 +285,54 @@ int ann_gated_ffn_backward(const void *dout_dev, int64_t ld_dout, const void *x_
         set_error("dx_dev must not overlap dout_dev or x_dev");
         return rc;
     }
-    const BackwardPlan plan = backward_plan(M, d_in, d_hidden, d_out, dtype);
+    const FfnPlan plan = ffn_plan(M, d_in, d_hidden, d_out, dtype, true);
     if (!ffn_workspace(workspace_dev, workspace_bytes, plan.total, &rc)) return rc;
     char *ws = (char *)workspace_dev;
     float *part = (float *)(ws + plan.part);
     void *dpre = ws + plan.dpre, *h = ws + plan.h;
+    Rows dout = {dout_dev, ld_dout}, x = {x_dev, ld_x}, w_in = {w_in_dev, d_in}, w_out = {w_out_dev, d_hidden};
+    const bool hidden = dx_dev || dw_in_dev || db_in_dev;  // the gradient of gate and up is wanted
     rc = ANN_OK;
-    if (dx_dev || dw_in_dev || db_in_dev || dw_out_dev) {
+    if (hidden || dw_out_dev) {
+        rc = ffn_rows(dtype, dout_dev, ld_dout, M, d_out, ws + plan.dout, plan.O8, s, &dout);
+        if (rc == ANN_OK) rc = ffn_rows(dtype, w_out_dev, d_hidden, d_out, d_hidden, ws + plan.w_out, plan.F8, s, &w_out);
         FfnProduct p = {};
         p.kind = dtype, p.epi = FFN_GRAD, p.a_rows = true, p.b_rows = false;
-        p.args.A = dout_dev, p.args.lda = ld_dout, p.args.B = w_out_dev, p.args.ldb = d_hidden;
+        p.args.A = dout.p, p.args.lda = dout.ld, p.args.B = w_out.p, p.args.ldb = w_out.ld;
         p.args.M = (int32_t)M, p.args.N = d_hidden, p.args.K = d_out;
-        p.args.C = dpre, p.args.ldc = (int64_t)2 * d_hidden, p.args.h = dw_out_dev ? h : nullptr;
+        p.args.C = dpre, p.args.ldc = plan.ld_pre, p.args.up = d_hidden, p.args.pad = dtype != ANN_F32;
+        p.args.h = dw_out_dev ? h : nullptr, p.args.ldh = plan.F8;
         p.args.pre = const_cast<float *>(pre_dev), p.args.act = act;
-        rc = launch_ffn_product(p, part, s);
+        if (rc == ANN_OK) rc = launch_ffn_product(p, part, s);
     }
     if (rc == ANN_OK && dx_dev) {
+        rc = ffn_rows(dtype, w_in_dev, d_in, (int64_t)2 * d_hidden, d_in, ws + plan.w_in, plan.D8, s, &w_in);
         FfnProduct p = {};
         p.kind = dtype, p.epi = FFN_STORE, p.a_rows = true, p.b_rows = false;
-        p.args.A = dpre, p.args.lda = (int64_t)2 * d_hidden, p.args.B = w_in_dev, p.args.ldb = d_in;
+        p.args.A = dpre, p.args.lda = plan.ld_pre, p.args.B = w_in.p, p.args.ldb = w_in.ld;
         p.args.M = (int32_t)M, p.args.N = d_in, p.args.K = 2 * d_hidden;
         p.args.C = dx_dev, p.args.ldc = ld_dx;
-        rc = launch_ffn_product(p, part, s);
+        if (rc == ANN_OK) rc = launch_ffn_product(p, part, s);
     }
     if (rc == ANN_OK && dw_in_dev) {
+        rc = ffn_rows(dtype, x_dev, ld_x, M, d_in, ws + plan.x, plan.D8, s, &x);
         FfnProduct p = {};
         p.kind = dtype, p.epi = FFN_STORE, p.a_rows = false, p.b_rows = false;
-        p.args.A = dpre, p.args.lda = (int64_t)2 * d_hidden, p.args.B = x_dev, p.args.ldb = ld_x;
+        p.args.A = dpre, p.args.lda = plan.ld_pre, p.args.B = x.p, p.args.ldb = x.ld;
         p.args.M = 2 * d_hidden, p.args.N = d_in, p.args.K = (int32_t)M;
         p.args.C = dw_in_dev, p.args.ldc = d_in;
-        rc = launch_ffn_product(p, part, s);
+        if (rc == ANN_OK) rc = launch_ffn_product(p, part, s);
     }
     if (rc == ANN_OK && dw_out_dev) {
         FfnProduct p = {};
         p.kind = dtype, p.epi = FFN_STORE, p.a_rows = false, p.b_rows = false;
-        p.args.A = dout_dev, p.args.lda = ld_dout, p.args.B = h, p.args.ldb = d_hidden;
+        p.args.A = dout.p, p.args.lda = dout.ld, p.args.B = h, p.args.ldb = plan.F8;
         p.args.M = d_out, p.args.N = d_hidden, p.args.K = (int32_t)M;
         p.args.C = dw_out_dev, p.args.ldc = d_hidden;
         rc = launch_ffn_product(p, part, s);
     }
     if (rc == ANN_OK && db_in_dev)
-        rc = launch_column_sum(dpre, M, (int64_t)2 * d_hidden, (int64_t)2 * d_hidden, dtype, db_in_dev, dtype, part, s);
+        rc = launch_column_sum(dpre, M, (int64_t)2 * d_hidden, plan.ld_pre, dtype, db_in_dev, dtype, part, s);
     if (rc == ANN_OK && db_out_dev) rc = launch_column_sum(dout_dev, M, d_out, ld_dout, dtype, db_out_dev, dtype, part, s);
     return rc;
 }

@@ -1,6 +1,6 @@
 // Column sums and fills shared by the operators on rows of vectors.  Sums are formed in fp32 in a fixed order (slices of
 // rows, then the slices one after the other), so that a result does not change from run to run.
-#include "rows.h"
+#include "ffn.h"
 
 namespace gmpgr {
 
@@ -117,6 +117,37 @@ int launch_column_sum(const void *in, int64_t M, int64_t n, int64_t ld, int in_d
         hipLaunchKernelGGL(column_sum_kernel<ANN_F16>, grid, dim3(256), 0, stream, (const _Float16 *)in, M, n, ld, part);
     ANN_HIP_TRY(hipGetLastError());
     return launch_sum_parts(part, P, n, out, dtype, stream);
+}
+
+// 8 elements a thread.
+__global__ void __launch_bounds__(256)
+pad_rows_kernel(const uint16_t *__restrict__ in, int64_t ld_in, int64_t rows, int64_t width, uint16_t *__restrict__ out, int64_t ld_out) {
+    typedef uint16_t u16x8 __attribute__((ext_vector_type(8)));
+    struct __attribute__((packed, aligned(2))) Pack {
+        u16x8 v;
+    };
+    const int64_t across = ld_out / 8, total = rows * across;
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
+        const int64_t r = i / across, c = (i - r * across) * 8, left = width - c;
+        const uint16_t *p = in + r * ld_in + c;
+        u16x8 v = {0, 0, 0, 0, 0, 0, 0, 0};
+        if (left >= 8) {
+            v = reinterpret_cast<const Pack *>(p)->v;
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                if (e < left) v[e] = p[e];
+        }
+        *(u16x8 *)(out + r * ld_out + c) = v;
+    }
+}
+
+int launch_pad_rows(const void *in, int64_t ld_in, int64_t rows, int64_t width, void *out, int64_t ld_out, hipStream_t stream) {
+    const int64_t groups = (rows * (ld_out / 8) + 255) / 256;
+    hipLaunchKernelGGL(pad_rows_kernel, dim3((unsigned)(groups < 8192 ? groups : 8192)), dim3(256), 0, stream,
+                       (const uint16_t *)in, ld_in, rows, width, (uint16_t *)out, ld_out);
+    ANN_HIP_TRY(hipGetLastError());
+    return ANN_OK;
 }
 
 }  // namespace gmpgr
