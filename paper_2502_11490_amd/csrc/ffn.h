@@ -194,16 +194,16 @@ struct FfnProduct {
     int kind, epi;
     bool a_rows, b_rows;
 };
-// How it is cut: tiles of tile x tile (FFN_GATE: half as many columns of C), k in `splits` slices.
+// How it is cut: tiles of rows x cols (FFN_GATE: half as many columns of C), k in `splits` slices.
 struct FfnCut {
-    int tile, splits;
+    int rows, cols, splits;
 };
 FfnCut ffn_cut(int kind, int64_t M, int64_t N, int64_t K, int epi);
 size_t ffn_part_floats(int kind, int64_t M, int64_t N, int64_t K, int epi);  // what launch_ffn_product needs as `part`
 int launch_ffn_product(const FfnProduct &p, float *part, hipStream_t stream);
 
 template <int KIND> int launch_ffn16(const FfnProduct &p, int tile, hipStream_t stream);  // ffn_bf16.hip, ffn_f16.hip
-int launch_ffn32(const FfnProduct &p, hipStream_t stream);                                // ffn_f32.hip
+int launch_ffn32(const FfnProduct &p, int cols, hipStream_t stream);                      // ffn_f32.hip
 
 // 16-bit operands as launch_ffn16 takes them: 16-byte aligned rows, the contiguous extent a multiple of 8, and 256 rows
 // within 2^30 bytes.

@@ -44,21 +44,31 @@ template <int KIND> static int launch_finish(const FfnArgs &a, int epi, hipStrea
     return ANN_OK;
 }
 
-// The cut that a simple account says is fastest: rounds of workgroups over 256 compute units (one of the 256 x 256 tiles a
-// unit, two of the others), each round as many steps of 64 k as a slice has, a round's start and end, and for slices the
-// writing and reading of the parts and one more launch.
+// The cut that a simple account says is fastest: rounds of workgroups over 256 compute units, each of which holds a_unit of
+// them, a round as many steps of 64 k as a slice has and a start and an end; a last round that leaves units with fewer
+// workgroups is that much shorter; and for slices the writing and reading of the parts and one more launch.
+struct FfnTileCost {
+    int rows, cols, a_unit;
+    double step, ends;  // microseconds of 64 k, of the start and the end, with a_unit of them at work (measured)
+};
+static const FfnTileCost FFN_TILES16[] = {{256, 256, 1, 1.7, 10.0}, {128, 128, 2, 1.1, 5.0}};
+static const FfnTileCost FFN_TILES32[] = {{128, 128, 2, 9.3, 6.0}, {64, 64, 4, 5.1, 5.0}};
+
 FfnCut ffn_cut(int kind, int64_t M, int64_t N, int64_t K, int epi) {
-    FfnCut best = {128, 1};
+    FfnCut best = {128, 128, 1};
     double least = 0.0;
-    for (int tile = 128; tile <= (kind == ANN_F32 ? 128 : 256); tile *= 2) {
-        const int64_t cols = epi == FFN_GATE ? tile / 2 : tile, tiles = ((M + tile - 1) / tile) * ((N + cols - 1) / cols);
-        const double step = kind == ANN_F32 ? 5.0 : tile == 256 ? 1.7 : 1.1, ends = tile == 256 ? 10.0 : 5.0;  // microseconds
+    for (int i = 0; i < 2; ++i) {
+        FfnTileCost c = kind == ANN_F32 ? FFN_TILES32[i] : FFN_TILES16[i];
+        if (c.rows == 64 && epi == FFN_GATE) c.rows = 128, c.a_unit = 2;  // gate and up of a column are one wave's
+        const int64_t cols = epi == FFN_GATE ? c.cols / 2 : c.cols, tiles = ((M + c.rows - 1) / c.rows) * ((N + cols - 1) / cols);
         for (int s = 1; s <= 16 && (s == 1 || s <= K / 256); s += s < 4 ? 1 : 2) {
-            const int64_t slots = tile == 256 ? 256 : 512, rounds = (tiles * s + slots - 1) / slots;
+            const int64_t slots = 256 * c.a_unit, groups = tiles * s, rounds = groups / slots, rest = groups % slots;
             const double steps = (double)((K + 64 * s - 1) / (64 * s));
-            double t = (double)rounds * (steps * step + ends);
+            double last = (double)((rest + 255) / 256) / c.a_unit;
+            if (rest > 0 && last < 1.0) last += 0.1;
+            double t = ((double)rounds + last) * steps * c.step + (double)(rounds + (rest > 0)) * c.ends;
             if (s > 1) t += 4.0 + 8.0 * s * (double)M * (double)N * (epi == FFN_GATE ? 2 : 1) / 4.0e6;
-            if (least == 0.0 || t < least) least = t, best = {tile, s};
+            if (least == 0.0 || t < least) least = t, best = {c.rows, c.cols, s};
         }
     }
     return best;
@@ -76,9 +86,9 @@ int launch_ffn_product(const FfnProduct &product, float *part, hipStream_t strea
     a.k_slice = cut.splits == 1 ? a.K : (int32_t)((((int64_t)a.K + cut.splits - 1) / cut.splits + 63) / 64 * 64);
     a.splits = (int32_t)(((int64_t)a.K + a.k_slice - 1) / a.k_slice);
     a.part = a.splits > 1 ? part : nullptr;
-    const int rc = p.kind == ANN_F32    ? launch_ffn32(p, stream)
-                   : p.kind == ANN_BF16 ? launch_ffn16<ANN_BF16>(p, cut.tile, stream)
-                                        : launch_ffn16<ANN_F16>(p, cut.tile, stream);
+    const int rc = p.kind == ANN_F32    ? launch_ffn32(p, cut.cols, stream)
+                   : p.kind == ANN_BF16 ? launch_ffn16<ANN_BF16>(p, cut.cols, stream)
+                                        : launch_ffn16<ANN_F16>(p, cut.cols, stream);
     if (rc != ANN_OK || a.splits == 1) return rc;
     return p.kind == ANN_F32    ? launch_finish<ANN_F32>(a, p.epi, stream)
            : p.kind == ANN_BF16 ? launch_finish<ANN_BF16>(a, p.epi, stream)
