@@ -24,7 +24,7 @@ struct FfnArgs {
     float *pre;           // [M][2 N]: FFN_GATE writes it (null = not), FFN_GRAD reads it
     void *h;              // [M][ldh], FFN_GRAD writes it (null = not)
     int64_t ldh;
-    bool pad;             // C's rows are padded to 8 columns for the next product: zeros go behind the last one
+    bool pad;             // C's rows are padded (to 8 columns) for the next product: zeros go behind the last column
     int32_t act;
     // sums over slices of k: slice s writes part[s][M][N or 2 N] in place of the epilogue
     float *part;
@@ -149,8 +149,10 @@ __device__ __forceinline__ void ffn_epilogue(const FfnArgs &p, int64_t m, int n,
         }
         ffn_act_each<KIND, W, false>(p.act, g, v, nullptr);
 #pragma unroll
-        for (int i = 0; i < W; ++i) v[i] = i < left ? v[i] * u[i] : 0.f;
-        store_cols<W>(C, p.pad ? W : left, v);
+        for (int i = 0; i < W; ++i) v[i] *= u[i];
+        store_cols<W>(C, left, v);
+        if (p.pad && left <= W)
+            for (int64_t i = p.N; i < p.ldc; ++i) ((T *)p.C + m * p.ldc)[i] = (T)0.f;
     } else {
         float a[W], slope[W];
         ffn_act_each<KIND, W, true>(p.act, r.gate, a, slope);
@@ -162,7 +164,7 @@ __device__ __forceinline__ void ffn_epilogue(const FfnArgs &p, int64_t m, int n,
         }
         store_cols<W>(C, left, v);
         store_cols<W>(C + p.up, left, w);
-        if (p.pad && left < W)
+        if (p.pad && left <= W)
             for (int64_t i = p.up + p.N; i < p.ldc; ++i) ((T *)p.C + m * p.ldc)[i] = (T)0.f;
         if (p.h) store_cols<W>((T *)p.h + m * p.ldh + n, left, a);
     }
@@ -204,6 +206,13 @@ int launch_ffn_product(const FfnProduct &p, float *part, hipStream_t stream);
 
 template <int KIND> int launch_ffn16(const FfnProduct &p, int tile, hipStream_t stream);  // ffn_bf16.hip, ffn_f16.hip
 int launch_ffn32(const FfnProduct &p, int cols, hipStream_t stream);                      // ffn_f32.hip
+
+// ffn_few.hip: the same for few rows, both operands' k contiguous, any alignment; FFN_STORE and FFN_GATE, no slices.
+// Up to how many rows that is the faster kernel: with N = 8192 gate columns and K = 2048 in bf16 16 us against 22 for 32
+// rows and 21 against 22 for 64; with N = 2048 and K = 8192 8.5 us against 16 for one row, 16.5 against 16 for 16 and 30
+// against 16 for 32 (too few workgroups, that read x over and over); in fp32 34 against 32 and 68 against 21 for 64.
+constexpr int ffn_few(int kind, int epi) { return epi == FFN_GATE && kind != ANN_F32 ? 64 : 16; }
+int launch_ffn_few(const FfnProduct &p, hipStream_t stream);
 
 // 16-bit operands as launch_ffn16 takes them: 16-byte aligned rows, the contiguous extent a multiple of 8, and 256 rows
 // within 2^30 bytes.

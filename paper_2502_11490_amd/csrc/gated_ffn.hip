@@ -1,5 +1,6 @@
 // The gated feed-forward block and its gradient: which products they are, how the products are cut, the workspace and the
-// C entry points.  The products are in ffn_mfma16.h and ffn_f32.hip.
+// C entry points.  The products are in ffn_mfma16.h, ffn_f32.hip and, for few rows,
+// ffn_few.hip.
 //
 //   forward : h = act(x w_in^T) (gate, up in one product, FFN_GATE), out = h w_out^T
 //   gradient: [dgate | dup], h from dout w_out (FFN_GRAD); dx = [dgate | dup] w_in; dw_in = [dgate | dup]^T x;
@@ -120,14 +121,16 @@ static FfnPlan ffn_plan(int64_t M, int64_t D, int64_t F, int64_t O, int dtype, b
     p.D8 = (D + to - 1) / to * to, p.F8 = (F + to - 1) / to * to, p.O8 = (O + to - 1) / to * to;
     p.ld_pre = (2 * F + to - 1) / to * to;
     p.h = r.take((size_t)M * p.F8 * e);
-    if (pack) {
+    const bool few_in = !gradient && M <= ffn_few(dtype, FFN_GATE), few_out = !gradient && M <= ffn_few(dtype, FFN_STORE);
+    if (pack && !few_in) {
         p.x = r.take((size_t)M * p.D8 * e);
         p.w_in = r.take((size_t)2 * F * p.D8 * e);
-        p.w_out = r.take((size_t)O * p.F8 * e);
     }
-    size_t n;
+    if (pack && !few_out) p.w_out = r.take((size_t)O * p.F8 * e);
+    size_t n = 0;
     if (!gradient) {
-        n = most(ffn_part_floats(dtype, M, F, D, FFN_GATE), ffn_part_floats(dtype, M, O, F, FFN_STORE));
+        if (!few_in) n = ffn_part_floats(dtype, M, F, D, FFN_GATE);
+        if (!few_out) n = most(n, ffn_part_floats(dtype, M, O, F, FFN_STORE));
     } else {
         if (pack) p.dout = r.take((size_t)M * p.O8 * e);
         p.dpre = r.take((size_t)M * p.ld_pre * e);
@@ -240,10 +243,16 @@ int ann_gated_ffn(const void *x_dev, int64_t ld_x, const void *w_in_dev, const v
     if (!ffn_workspace(workspace_dev, workspace_bytes, plan.total, &rc)) return rc;
     char *ws = (char *)workspace_dev;
     hipStream_t s = (hipStream_t)stream;
-    Rows x, w_in, w_out;
-    rc = ffn_rows(dtype, x_dev, ld_x, M, d_in, ws + plan.x, plan.D8, s, &x);
-    if (rc == ANN_OK) rc = ffn_rows(dtype, w_in_dev, d_in, (int64_t)2 * d_hidden, d_in, ws + plan.w_in, plan.D8, s, &w_in);
-    if (rc == ANN_OK) rc = ffn_rows(dtype, w_out_dev, d_hidden, d_out, d_hidden, ws + plan.w_out, plan.F8, s, &w_out);
+    const bool few_in = M <= ffn_few(dtype, FFN_GATE), few_out = M <= ffn_few(dtype, FFN_STORE);
+    Rows x = {x_dev, ld_x}, w_in = {w_in_dev, d_in}, w_out = {w_out_dev, d_hidden};
+    rc = ANN_OK;
+    if (!few_in) {
+        rc = ffn_rows(dtype, x_dev, ld_x, M, d_in, ws + plan.x, plan.D8, s, &x);
+        if (rc == ANN_OK)
+            rc = ffn_rows(dtype, w_in_dev, d_in, (int64_t)2 * d_hidden, d_in, ws + plan.w_in, plan.D8, s, &w_in);
+    }
+    if (!few_out && rc == ANN_OK)
+        rc = ffn_rows(dtype, w_out_dev, d_hidden, d_out, d_hidden, ws + plan.w_out, plan.F8, s, &w_out);
     if (rc != ANN_OK) return rc;
     FfnProduct p = {};
     p.kind = dtype, p.epi = FFN_GATE, p.a_rows = true, p.b_rows = true;
@@ -251,14 +260,14 @@ int ann_gated_ffn(const void *x_dev, int64_t ld_x, const void *w_in_dev, const v
     p.args.M = (int32_t)M, p.args.N = d_hidden, p.args.K = d_in, p.args.up = d_hidden;
     p.args.C = ws + plan.h, p.args.ldc = plan.F8, p.args.pad = dtype != ANN_F32;
     p.args.bias = b_in_dev, p.args.pre = pre_dev, p.args.act = act;
-    rc = launch_ffn_product(p, (float *)(ws + plan.part), s);
+    rc = few_in ? launch_ffn_few(p, s) : launch_ffn_product(p, (float *)(ws + plan.part), s);
     if (rc != ANN_OK) return rc;
     FfnProduct q = {};
     q.kind = dtype, q.epi = FFN_STORE, q.a_rows = true, q.b_rows = true;
     q.args.A = ws + plan.h, q.args.lda = plan.F8, q.args.B = w_out.p, q.args.ldb = w_out.ld;
     q.args.M = (int32_t)M, q.args.N = d_out, q.args.K = d_hidden;
     q.args.C = out_dev, q.args.ldc = ld_out, q.args.bias = b_out_dev;
-    return launch_ffn_product(q, (float *)(ws + plan.part), s);
+    return few_out ? launch_ffn_few(q, s) : launch_ffn_product(q, (float *)(ws + plan.part), s);
 }
 
 int ann_gated_ffn_backward(const void *dout_dev, int64_t ld_dout, const void *x_dev, int64_t ld_x, const float *pre_dev,
