@@ -693,32 +693,27 @@ def _dense(t: Optional[torch.Tensor], name: str, x: torch.Tensor, shape, dtype=N
     return t.data_ptr()
 
 
-class _Here:
-    """The current device and stream are the call's."""
-
-    def __enter__(self):
-        return None
-
-    def __exit__(self, *a):
-        return False
-
-
-_HERE_ALREADY = _Here()
-
-
 def _place(x: torch.Tensor, stream):
-    """What makes x's device, and `stream` where one is given, the current ones while a call allocates and launches."""
-    if not x.is_cuda:
-        raise ValueError("the rows must be a device tensor")
+    """What makes x's device, and `stream` where one is given, the current ones while a call allocates and launches;
+    None where they are that already (the usual case, which entering a context would lengthen by microseconds)."""
     if stream is not None:
         if stream.device != x.device:
             raise ValueError(f"stream is on {stream.device}, the rows are on {x.device}")
         return torch.cuda.stream(stream)
-    return _HERE_ALREADY if torch.cuda.current_device() == x.device.index else torch.cuda.device(x.device)
+    if not x.is_cuda or torch._C._cuda_getDevice() == x.get_device():
+        return None
+    return torch.cuda.device(x.device)
 
 
-def _row_workspace(workspace: Optional[torch.Tensor], need: int, x: torch.Tensor):
-    """(pointer, bytes) of the caller's workspace or of a fresh one, and the tensor that keeps it."""
+def _current(x: torch.Tensor) -> int:
+    """The current stream of x's device as the library takes it."""
+    if not x.is_cuda:
+        raise ValueError("the rows must be a device tensor")
+    return torch._C._cuda_getCurrentRawStream(x.get_device())
+
+
+def _row_workspace(workspace: Optional[torch.Tensor], need: int, x: torch.Tensor) -> torch.Tensor:
+    """The caller's workspace, or a fresh one."""
     if need == 0:
         raise AnnError(ANN_EINVAL, ann_last_error())
     if workspace is None:
@@ -732,21 +727,23 @@ def ann_layer_norm(x: torch.Tensor, gamma: Optional[torch.Tensor] = None, beta: 
                    eps: float = 1e-5, save: bool = False, out: Optional[torch.Tensor] = None, stream=None):
     """Layer norm over the last dimension of x [..., d]; gamma, beta [d] of x's type (None = ones, zeros).  `out` may be
     x.  With save=True (out, mean, rstd), the last two fp32 [rows], for ann_layer_norm_backward."""
+    place = _place(x, stream)
+    if place is not None:
+        with place:
+            return ann_layer_norm(x, gamma, beta, eps, save, out)
     code = _row_code(x, "x")
     M, d, ld = _row_shape(x, "x")
     gp, bp = _dense(gamma, "gamma", x, (d,)), _dense(beta, "beta", x, (d,))
-    if out is not None:
+    if out is None:
+        out, ld_out = torch.empty(x.shape, dtype=x.dtype, device=x.device), d
+    else:
         _like(out, "out", x, x.shape)
         ld_out = _row_shape(out, "out")[2]
-    with _place(x, stream):
-        if out is None:
-            out, ld_out = torch.empty(x.shape, dtype=x.dtype, device=x.device), d
-        mean = rstd = None
-        if save:
-            mean, rstd = torch.empty((2, M), dtype=torch.float32, device=x.device)
-        rc = load_library().ann_layer_norm(x.data_ptr(), ld, gp, bp, M, d, code, eps, out.data_ptr(), ld_out,
-                                           mean.data_ptr() if save else None, rstd.data_ptr() if save else None,
-                                           torch.cuda.current_stream().cuda_stream)
+    mean = rstd = mp = rp = None
+    if save:
+        mean, rstd = torch.empty((2, M), dtype=torch.float32, device=x.device)
+        mp, rp = mean.data_ptr(), rstd.data_ptr()
+    rc = load_library().ann_layer_norm(x.data_ptr(), ld, gp, bp, M, d, code, eps, out.data_ptr(), ld_out, mp, rp, _current(x))
     if rc:
         _check(rc)
     return (out, mean, rstd) if save else out
@@ -763,6 +760,10 @@ def ann_layer_norm_backward(dout: torch.Tensor, x: torch.Tensor, gamma: Optional
                             rstd: torch.Tensor, need_dx: bool = True, need_dparams: bool = True,
                             workspace: Optional[torch.Tensor] = None, stream=None):
     """(dx, dgamma, dbeta) of ann_layer_norm(x, gamma, beta, save=True); None for what is not needed."""
+    place = _place(x, stream)
+    if place is not None:
+        with place:
+            return ann_layer_norm_backward(dout, x, gamma, mean, rstd, need_dx, need_dparams, workspace)
     code = _row_code(x, "x")
     M, d, ld = _row_shape(x, "x")
     _like(dout, "dout", x, x.shape)
@@ -770,23 +771,19 @@ def ann_layer_norm_backward(dout: torch.Tensor, x: torch.Tensor, gamma: Optional
     gp = _dense(gamma, "gamma", x, (d,))
     mp, rp = _dense(mean, "mean", x, (M,), torch.float32), _dense(rstd, "rstd", x, (M,), torch.float32)
     lib = load_library()
-    with _place(x, stream):
-        dx = dparams = None
-        wp, wb = None, 0
-        if need_dx:
-            dx = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-        if need_dparams:
-            dparams = torch.empty((2, d), dtype=x.dtype, device=x.device)
-            workspace = _row_workspace(workspace, lib.ann_layer_norm_backward_workspace_bytes(M, d, code), x)
-            wp, wb = workspace.data_ptr(), workspace.numel()
-        dg = dparams.data_ptr() if need_dparams else None
-        rc = lib.ann_layer_norm_backward(dout.data_ptr(), ld_dout, x.data_ptr(), ld, gp, mp, rp, M, d, code,
-                                         dx.data_ptr() if need_dx else None, d, dg,
-                                         dg + d * x.element_size() if need_dparams else None, wp, wb,
-                                         torch.cuda.current_stream().cuda_stream)
+    dx = dgamma = dbeta = dgp = dbp = wp = None
+    wb = 0
+    if need_dx:
+        dx = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    if need_dparams:
+        dgamma, dbeta = torch.empty((2, d), dtype=x.dtype, device=x.device)
+        workspace = _row_workspace(workspace, lib.ann_layer_norm_backward_workspace_bytes(M, d, code), x)
+        dgp, dbp, wp, wb = dgamma.data_ptr(), dbeta.data_ptr(), workspace.data_ptr(), workspace.numel()
+    rc = lib.ann_layer_norm_backward(dout.data_ptr(), ld_dout, x.data_ptr(), ld, gp, mp, rp, M, d, code,
+                                     dx.data_ptr() if need_dx else None, d, dgp, dbp, wp, wb, _current(x))
     if rc:
         _check(rc)
-    return (dx, dparams[0], dparams[1]) if need_dparams else (dx, None, None)
+    return dx, dgamma, dbeta
 
 
 def ann_dropout(x: torch.Tensor, p: float, seed: int, draw: int = 0, residual: Optional[torch.Tensor] = None,
@@ -794,21 +791,25 @@ def ann_dropout(x: torch.Tensor, p: float, seed: int, draw: int = 0, residual: O
     """residual + dropout of x (None = no residual), the choice a pure function of (seed, draw, element): the gradient
     of x is ann_dropout(dout, p, seed, draw).  Contiguous tensors of one shape; `out` may be x or residual.  draw_dev
     (one int64 on the device) is added to `draw` when the kernel runs: the replays of a recorded call draw anew."""
+    place = _place(x, stream)
+    if place is not None:
+        with place:
+            return ann_dropout(x, p, seed, draw, residual, out, draw_dev)
     code = _row_code(x, "x")
     if not x.is_contiguous():
         raise ValueError("x must be contiguous")
     rp = _dense(residual, "residual", x, x.shape)
-    op = _dense(out, "out", x, x.shape)
-    if draw_dev is not None and (draw_dev.numel() != 1 or draw_dev.device != x.device or
-                                 draw_dev.dtype not in (torch.int64, torch.uint64)):
-        raise ValueError(f"draw_dev must be one int64 on {x.device}")
-    with _place(x, stream):
-        if out is None:
-            out = torch.empty_like(x)
-            op = out.data_ptr()
-        rc = load_library().ann_dropout(x.data_ptr(), rp, op, x.numel(), code, p, seed, draw,
-                                        draw_dev.data_ptr() if draw_dev is not None else None,
-                                        torch.cuda.current_stream().cuda_stream)
+    dp = None
+    if draw_dev is not None:
+        if draw_dev.numel() != 1 or draw_dev.device != x.device or draw_dev.dtype not in (torch.int64, torch.uint64):
+            raise ValueError(f"draw_dev must be one int64 on {x.device}")
+        dp = draw_dev.data_ptr()
+    if out is None:
+        out = torch.empty_like(x)
+        op = out.data_ptr()
+    else:
+        op = _dense(out, "out", x, x.shape)
+    rc = load_library().ann_dropout(x.data_ptr(), rp, op, x.numel(), code, p, seed, draw, dp, _current(x))
     if rc:
         _check(rc)
     return out
@@ -837,21 +838,23 @@ def ann_gated_ffn(x: torch.Tensor, w_in: torch.Tensor, w_out: torch.Tensor, b_in
     """(act(gate) * up) w_out^T + b_out with [gate | up] = x w_in^T + b_in: x [..., d_in], w_in [2 * d_hidden][d_in] (the gate's
     rows first), w_out [d_out][d_hidden], all of one type.  With save=True (out, pre), pre [rows][2 * d_hidden] fp32, for
     ann_gated_ffn_backward."""
+    place = _place(x, stream)
+    if place is not None:
+        with place:
+            return ann_gated_ffn(x, w_in, w_out, b_in, b_out, act, save, out, workspace)
     code, M, D, F, O, ld, wip, wop = _ffn_shapes(x, w_in, w_out)
     bip, bop = _dense(b_in, "b_in", x, (2 * F,)), _dense(b_out, "b_out", x, (O,))
     shape, ld_out = x.shape[:-1] + (O,), O
-    if out is not None:
+    if out is None:
+        out = torch.empty(shape, dtype=x.dtype, device=x.device)
+    else:
         _like(out, "out", x, shape)
         ld_out = _row_shape(out, "out")[2]
     lib = load_library()
-    with _place(x, stream):
-        if out is None:
-            out = torch.empty(shape, dtype=x.dtype, device=x.device)
-        pre = torch.empty((M, 2 * F), dtype=torch.float32, device=x.device) if save else None
-        workspace = _row_workspace(workspace, lib.ann_gated_ffn_workspace_bytes(M, D, F, O, code), x)
-        rc = lib.ann_gated_ffn(x.data_ptr(), ld, wip, bip, wop, bop, M, D, F, O, act, code, out.data_ptr(), ld_out,
-                               pre.data_ptr() if save else None, workspace.data_ptr(), workspace.numel(),
-                               torch.cuda.current_stream().cuda_stream)
+    pre = torch.empty((M, 2 * F), dtype=torch.float32, device=x.device) if save else None
+    workspace = _row_workspace(workspace, lib.ann_gated_ffn_workspace_bytes(M, D, F, O, code), x)
+    rc = lib.ann_gated_ffn(x.data_ptr(), ld, wip, bip, wop, bop, M, D, F, O, act, code, out.data_ptr(), ld_out,
+                           pre.data_ptr() if save else None, workspace.data_ptr(), workspace.numel(), _current(x))
     if rc:
         _check(rc)
     return (out, pre) if save else out
@@ -869,21 +872,24 @@ def ann_gated_ffn_backward(dout: torch.Tensor, x: torch.Tensor, pre: torch.Tenso
                            need_dw: bool = True, workspace: Optional[torch.Tensor] = None, stream=None):
     """(dx, dw_in, dw_out, db_in, db_out) of ann_gated_ffn(..., save=True); None for what is not needed (the last two
     are given with bias=True)."""
+    place = _place(x, stream)
+    if place is not None:
+        with place:
+            return ann_gated_ffn_backward(dout, x, pre, w_in, w_out, act, bias, need_dx, need_dw, workspace)
     code, M, D, F, O, ld, wip, wop = _ffn_shapes(x, w_in, w_out)
     _like(dout, "dout", x, x.shape[:-1] + (O,))
     ld_dout = _row_shape(dout, "dout")[2]
     pp = _dense(pre, "pre", x, (M, 2 * F), torch.float32)
     lib = load_library()
-    with _place(x, stream):
-        new = lambda *shape: torch.empty(shape, dtype=x.dtype, device=x.device)  # noqa: E731
-        dx = torch.empty(x.shape, dtype=x.dtype, device=x.device) if need_dx else None
-        dw_in, dw_out = (new(2 * F, D), new(O, F)) if need_dw else (None, None)
-        db_in, db_out = (new(2 * F), new(O)) if bias else (None, None)
-        workspace = _row_workspace(workspace, lib.ann_gated_ffn_backward_workspace_bytes(M, D, F, O, code), x)
-        ptr = lambda t: None if t is None else t.data_ptr()  # noqa: E731
-        rc = lib.ann_gated_ffn_backward(dout.data_ptr(), ld_dout, x.data_ptr(), ld, pp, wip, wop, M, D, F, O, act, code,
-                                        ptr(dx), D, ptr(dw_in), ptr(db_in), ptr(dw_out), ptr(db_out),
-                                        workspace.data_ptr(), workspace.numel(), torch.cuda.current_stream().cuda_stream)
+    new = lambda *shape: torch.empty(shape, dtype=x.dtype, device=x.device)  # noqa: E731
+    dx = new(*x.shape) if need_dx else None
+    dw_in, dw_out = (new(2 * F, D), new(O, F)) if need_dw else (None, None)
+    db_in, db_out = (new(2 * F), new(O)) if bias else (None, None)
+    workspace = _row_workspace(workspace, lib.ann_gated_ffn_backward_workspace_bytes(M, D, F, O, code), x)
+    ptr = lambda t: None if t is None else t.data_ptr()  # noqa: E731
+    rc = lib.ann_gated_ffn_backward(dout.data_ptr(), ld_dout, x.data_ptr(), ld, pp, wip, wop, M, D, F, O, act, code,
+                                    ptr(dx), D, ptr(dw_in), ptr(db_in), ptr(dw_out), ptr(db_out),
+                                    workspace.data_ptr(), workspace.numel(), _current(x))
     if rc:
         _check(rc)
     return dx, dw_in, dw_out, db_in, db_out

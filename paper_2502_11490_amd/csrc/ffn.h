@@ -107,20 +107,29 @@ template <int W, typename T> __device__ __forceinline__ void store_cols(T *p, in
 template <int W> struct FfnRow {
     float gate[W], up[W];
 };
-template <int W, int EPI> __device__ __forceinline__ void ffn_row(const FfnArgs &p, int64_t m, int n, FfnRow<W> &r) {
+template <int W, int EPI, bool INSIDE = false>
+__device__ __forceinline__ void ffn_row(const FfnArgs &p, int64_t m, int n, FfnRow<W> &r) {
     if (EPI == FFN_GRAD) {
-        const float *q = p.pre + m * 2 * p.N + n;
-        load_cols<W>(q, p.N - n, r.gate);
-        load_cols<W>(q + p.N, p.N - n, r.up);
+        const float *__restrict__ q = p.pre + m * 2 * p.N + n;
+        load_cols<W>(q, INSIDE ? W : p.N - n, r.gate);
+        load_cols<W>(q + p.N, INSIDE ? W : p.N - n, r.up);
     }
 }
 
-// W consecutive columns from n on of row m (the caller has m < M, n < N); `up` for FFN_GATE only.
-template <int KIND, int EPI, int W>
+struct FfnTrue {
+    static constexpr bool value = true;
+};
+struct FfnFalse {
+    static constexpr bool value = false;
+};
+
+// W consecutive columns from n on of row m (the caller has m < M, n < N); `up` for FFN_GATE only.  INSIDE: all of the
+// tile's columns are inside, so that nothing is padded either.
+template <int KIND, int EPI, int W, bool INSIDE = false>
 __device__ __forceinline__ void ffn_epilogue(const FfnArgs &p, int64_t m, int n, const float *sum, const float *up,
                                              const FfnRow<W> &r) {
     using T = typename ElemOf<KIND>::type;
-    const int left = p.N - n;
+    const int left = INSIDE ? W : p.N - n;
     T *C = (T *)p.C + m * p.ldc + n;
     float v[W], w[W];
     if (EPI == FFN_STORE) {
@@ -151,7 +160,7 @@ __device__ __forceinline__ void ffn_epilogue(const FfnArgs &p, int64_t m, int n,
 #pragma unroll
         for (int i = 0; i < W; ++i) v[i] *= u[i];
         store_cols<W>(C, left, v);
-        if (p.pad && left <= W)
+        if (!INSIDE && p.pad && left <= W)
             for (int64_t i = p.N; i < p.ldc; ++i) ((T *)p.C + m * p.ldc)[i] = (T)0.f;
     } else {
         float a[W], slope[W];
@@ -164,7 +173,7 @@ __device__ __forceinline__ void ffn_epilogue(const FfnArgs &p, int64_t m, int n,
         }
         store_cols<W>(C, left, v);
         store_cols<W>(C + p.up, left, w);
-        if (p.pad && left <= W)
+        if (!INSIDE && p.pad && left <= W)
             for (int64_t i = p.up + p.N; i < p.ldc; ++i) ((T *)p.C + m * p.ldc)[i] = (T)0.f;
         if (p.h) store_cols<W>((T *)p.h + m * p.ldh + n, left, a);
     }
@@ -219,7 +228,16 @@ int launch_ffn_few(const FfnProduct &p, hipStream_t stream);
 inline bool ffn_direct(const void *p, int64_t ld, int64_t width) {
     return (uintptr_t)p % 16 == 0 && ld % 8 == 0 && width % 8 == 0 && ld <= (int64_t)1 << 21;
 }
-// rows.hip: out [rows][ld_out] = in [rows][width], zeros in the columns behind; 16-bit elements
-int launch_pad_rows(const void *in, int64_t ld_in, int64_t rows, int64_t width, void *out, int64_t ld_out, hipStream_t stream);
+// rows.hip: up to four copies out [rows][ld_out] = in [rows][width], zeros in the columns behind, of 16-bit elements, in one launch
+struct PadRows {
+    struct Item {
+        const void *in;
+        int64_t ld_in, rows, width;
+        void *out;
+        int64_t ld_out;
+    } item[4];
+    int n;
+};
+int launch_pad_rows(const PadRows &p, hipStream_t stream);
 
 }  // namespace gmpgr

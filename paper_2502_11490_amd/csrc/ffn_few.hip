@@ -134,8 +134,9 @@ template <int KIND, int EPI> static int launch_few_rows(const FfnArgs &a, hipStr
     if (a.M <= 8) return launch_few<KIND, EPI, 2, 1, 1>(a, stream);
     if (a.M <= 16) return launch_few<KIND, EPI, 1, 1, 1>(a, stream);
     if constexpr (ffn_few(KIND, EPI) > 16) {
-        if (a.M <= 32) return launch_few<KIND, EPI, 1, 2, 2>(a, stream);
-        return launch_few<KIND, EPI, 1, 4, 2>(a, stream);
+        // 32 columns a workgroup, which read x half as often, where that still occupies every compute unit
+        if (a.N < 32 * 256) return a.M <= 32 ? launch_few<KIND, EPI, 1, 2, 1>(a, stream) : launch_few<KIND, EPI, 1, 4, 1>(a, stream);
+        return a.M <= 32 ? launch_few<KIND, EPI, 1, 2, 2>(a, stream) : launch_few<KIND, EPI, 1, 4, 2>(a, stream);
     }
     set_error("%d rows are too many for this kernel", a.M);
     return ANN_EINVAL;

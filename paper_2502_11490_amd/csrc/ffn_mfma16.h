@@ -203,61 +203,76 @@ __global__ void __launch_bounds__(256, BM == 256 ? 1 : 2) ffn_mfma16_kernel(FfnA
         for (int j = 0; j < NT; ++j) asm volatile("" : "+a"(acc[i][j]));
     __builtin_amdgcn_sched_barrier(0);
 
-    // The sums go through LDS, half of the wave's rows at a time and each wave in a part of its own, and from there 8 columns
-    // a lane, row after row, to the epilogue: the instruction leaves 4 columns of 16 rows in a lane, which would be
-    // pieces of 8 bytes of 16 lines a store.  Piece q (4 columns) of row r lies at q ^ (r & 15).
+    // The sums go through LDS, half of the wave's rows at a time and each wave in a part of its own, and from there row after
+    // row to the epilogue, a lane 4 columns of either half of the row's: the instruction leaves 4 columns of 16 rows in a
+    // lane, which would be pieces of 8 bytes of 16 lines a store; so a line is one access's.  Piece q (4 columns) of row r
+    // lies at q ^ (r & 15).
     __syncthreads();
     constexpr int WN = BN / 2, HALF = MT / 2 * 16;
     constexpr int WIDE = GATE ? WN / 2 : WN, LANES = WIDE / 8, ROWS = 64 / LANES;  // columns of C, lanes a row, rows at a time
     float *const mine = (float *)lds + wave * HALF * WN;
-    const int lane_row = lane / LANES, c = (lane % LANES) * 8;                     // c: first of the lane's columns
+    const int lane_row = lane / LANES, c = (lane % LANES) * 4;                     // c: first of the lane's columns
     const int n = n0 + (GATE ? wn / 2 : wn) + c;
-    const int q0 = GATE ? (c >> 4) * 8 + (c & 15) / 4 : c / 4;                     // GATE: 16 columns of the gate, 16 of up, ...
+    // the piece of column c + e WIDE / 2; GATE: 16 columns of the gate, 16 of up, ...
+    auto piece = [&](int e) { const int at = c + e * (WIDE / 2); return GATE ? (at >> 4) * 8 + (at & 15) / 4 : at / 4; };
+    // What the epilogue reads of memory is on its way one batch of rows ahead.  A tile inside C asks nothing per lane: with a
+    // test the compiler would wait for each load where the branches meet.
+    constexpr int AHEAD = HALF / ROWS < 4 ? HALF / ROWS : 4;
+    auto finish = [&](auto inside) {
+        constexpr bool INSIDE = decltype(inside)::value;
 #pragma unroll
-    for (int half = 0; half < 2; ++half) {
+        for (int half = 0; half < 2; ++half) {
 #pragma unroll
-        for (int i = 0; i < MT / 2; ++i)
+            for (int i = 0; i < MT / 2; ++i)
 #pragma unroll
-            for (int j = 0; j < NT; ++j)
-                *(f32x4 *)(mine + (i * 16 + (lane & 15)) * WN + ((j * 4 + (lane >> 4)) ^ (lane & 15)) * 4) =
-                    acc[half * (MT / 2) + i][j];
-        const int64_t m_first = m0 + wm + half * HALF;
-        constexpr int AHEAD = HALF / ROWS < 4 ? HALF / ROWS : 4;  // rows whose gate and up values are on their way together
-        for (int r0 = 0; r0 < HALF; r0 += ROWS * AHEAD) {
-            FfnRow<8> row[AHEAD];
+                for (int j = 0; j < NT; ++j)
+                    *(f32x4 *)(mine + (i * 16 + (lane & 15)) * WN + ((j * 4 + (lane >> 4)) ^ (lane & 15)) * 4) =
+                        acc[half * (MT / 2) + i][j];
+            const int64_t m_first = m0 + wm + half * HALF + lane_row;
+            FfnRow<4> row[AHEAD][2], next[AHEAD][2];
+            auto fetch = [&](int r0) {
 #pragma unroll
-            for (int x = 0; x < AHEAD; ++x) {
-                const int64_t m = m_first + r0 + x * ROWS + lane_row;
-                if (EPI == FFN_GRAD && !p.part && m < p.M && n < p.N) ffn_row<8, EPI>(p, m, n, row[x]);
-            }
+                for (int x = 0; x < AHEAD; ++x)
 #pragma unroll
-            for (int x = 0; x < AHEAD; ++x) {
-                const int r = r0 + x * ROWS + lane_row;
-                const int64_t m = m_first + r;
-                if (m >= p.M || n >= p.N) continue;
-                float s[8], u[8];
-#pragma unroll
-                for (int e = 0; e < 2; ++e) {
-                    const f32x4 v = *(const f32x4 *)(mine + r * WN + ((q0 + e) ^ (r & 15)) * 4);
-#pragma unroll
-                    for (int f = 0; f < 4; ++f) s[e * 4 + f] = v[f], u[e * 4 + f] = 0.f;
-                    if (GATE) {
-                        const f32x4 w = *(const f32x4 *)(mine + r * WN + ((q0 + 4 + e) ^ (r & 15)) * 4);
-#pragma unroll
-                        for (int f = 0; f < 4; ++f) u[e * 4 + f] = w[f];
+                    for (int e = 0; e < 2; ++e) {
+                        const int64_t m = m_first + r0 + x * ROWS;
+                        const int ne = n + e * (WIDE / 2);
+                        if (EPI == FFN_GRAD && (INSIDE || (!p.part && m < p.M && ne < p.N)))
+                            ffn_row<4, EPI, INSIDE>(p, m, ne, next[x][e]);
                     }
-                }
-                if (p.part) {
-                    const int64_t width = GATE ? 2 * (int64_t)p.N : p.N;
-                    float *o = p.part + ((int64_t)t.split * p.M + m) * width + n;
-                    store_cols<8>(o, p.N - n, s);
-                    if (GATE) store_cols<8>(o + p.N, p.N - n, u);
-                } else {
-                    ffn_epilogue<KIND, EPI, 8>(p, m, n, s, u, row[x]);
-                }
+            };
+            fetch(0);
+            for (int r0 = 0; r0 < HALF; r0 += ROWS * AHEAD) {
+#pragma unroll
+                for (int x = 0; x < AHEAD; ++x) row[x][0] = next[x][0], row[x][1] = next[x][1];
+                if (r0 + ROWS * AHEAD < HALF) fetch(r0 + ROWS * AHEAD);
+#pragma unroll
+                for (int x = 0; x < AHEAD; ++x)
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        const int r = r0 + x * ROWS + lane_row, ne = n + e * (WIDE / 2);
+                        const int64_t m = m_first + r0 + x * ROWS;
+                        if (!INSIDE && (m >= p.M || ne >= p.N)) continue;
+                        const f32x4 v = *(const f32x4 *)(mine + r * WN + (piece(e) ^ (r & 15)) * 4);
+                        f32x4 w = f32x4{0.f, 0.f, 0.f, 0.f};
+                        if (GATE) w = *(const f32x4 *)(mine + r * WN + ((piece(e) + 4) ^ (r & 15)) * 4);
+                        const float s[4] = {v[0], v[1], v[2], v[3]}, u[4] = {w[0], w[1], w[2], w[3]};
+                        if (!INSIDE && p.part) {
+                            const int64_t width = GATE ? 2 * (int64_t)p.N : p.N;
+                            float *o = p.part + ((int64_t)t.split * p.M + m) * width + ne;
+                            store_cols<4>(o, p.N - ne, s);
+                            if (GATE) store_cols<4>(o + p.N, p.N - ne, u);
+                        } else {
+                            ffn_epilogue<KIND, EPI, 4, INSIDE>(p, m, ne, s, u, row[x][e]);
+                        }
+                    }
             }
         }
-    }
+    };
+    if (m0 + BM <= p.M && n0 + COLS <= p.N && !p.part)
+        finish(FfnTrue{});
+    else
+        finish(FfnFalse{});
 #endif
 }
 

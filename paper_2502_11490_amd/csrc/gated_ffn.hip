@@ -47,13 +47,15 @@ template <int KIND> static int launch_finish(const FfnArgs &a, int epi, hipStrea
 
 // The cut that a simple account says is fastest: rounds of workgroups over 256 compute units, each of which holds a_unit of
 // them, a round as many steps of 64 k as a slice has and a start and an end; a last round that leaves units with fewer
-// workgroups is that much shorter; and for slices the writing and reading of the parts and one more launch.
+// workgroups is that much shorter; and for slices the writing and reading of the parts and one more launch.  Fitted to
+// measured products: of 8192 x 8192 x 2048 (FFN_GRAD) 442 us in tiles of 256, 472 in tiles of 128; 4096 x 2048 x 512
+// (FFN_GATE) 32 and 28; 4096 x 2048 x 2048 (FFN_STORE) 52 and 34; 8192 x 2048 x 16384 (FFN_STORE) 448 and 550.
 struct FfnTileCost {
     int rows, cols, a_unit;
-    double step, ends;  // microseconds of 64 k, of the start and the end, with a_unit of them at work (measured)
+    double step, ends[3];  // microseconds of 64 k, of the start and the end by epilogue, with a_unit of them at work
 };
-static const FfnTileCost FFN_TILES16[] = {{256, 256, 1, 1.7, 10.0}, {128, 128, 2, 1.1, 5.0}};
-static const FfnTileCost FFN_TILES32[] = {{128, 128, 2, 9.3, 6.0}, {64, 64, 4, 5.1, 5.0}};
+static const FfnTileCost FFN_TILES16[] = {{256, 256, 1, 1.7, {13.0, 17.0, 50.0}}, {128, 128, 2, 1.1, {4.0, 6.0, 20.0}}};
+static const FfnTileCost FFN_TILES32[] = {{128, 128, 2, 9.3, {6.0, 6.0, 12.0}}, {64, 64, 4, 5.1, {5.0, 5.0, 10.0}}};
 
 FfnCut ffn_cut(int kind, int64_t M, int64_t N, int64_t K, int epi) {
     FfnCut best = {128, 128, 1};
@@ -67,8 +69,9 @@ FfnCut ffn_cut(int kind, int64_t M, int64_t N, int64_t K, int epi) {
             const double steps = (double)((K + 64 * s - 1) / (64 * s));
             double last = (double)((rest + 255) / 256) / c.a_unit;
             if (rest > 0 && last < 1.0) last += 0.1;
-            double t = ((double)rounds + last) * steps * c.step + (double)(rounds + (rest > 0)) * c.ends;
-            if (s > 1) t += 4.0 + 8.0 * s * (double)M * (double)N * (epi == FFN_GATE ? 2 : 1) / 4.0e6;
+            double t = ((double)rounds + last) * steps * c.step + (double)(rounds + (rest > 0)) * c.ends[s > 1 ? FFN_STORE : epi];
+            if (s > 1)  // the parts come out of the caches, what the epilogue reads and writes does not
+                t += 4.0 + (double)M * (double)N * (8.0 * s * (epi == FFN_GATE ? 2 : 1) / 1.0e7 + (epi == FFN_STORE ? 0.0 : 12.0 / 4.0e6));
             if (least == 0.0 || t < least) least = t, best = {c.rows, c.cols, s};
         }
     }
@@ -138,27 +141,22 @@ static FfnPlan ffn_plan(int64_t M, int64_t D, int64_t F, int64_t O, int dtype, b
         n = most(n, ffn_part_floats(dtype, M, D, 2 * F, FFN_STORE));
         n = most(n, ffn_part_floats(dtype, 2 * F, D, M, FFN_STORE));
         n = most(n, ffn_part_floats(dtype, O, F, M, FFN_STORE));
-        n = most(n, (size_t)column_sum_parts(M, 2 * F) * 2 * F);
-        n = most(n, (size_t)column_sum_parts(M, O) * O);
+        n = most(n, (size_t)column_sum_parts(M, 2 * F + O) * (2 * F + O));
     }
     p.part = r.take(sizeof(float) * n);
     p.total = r.total + 256;
     return p;
 }
 
-// An operand as the product's kernels take it: itself, or its copy in the workspace.
+// An operand as the product's kernels take it: itself, or its copy in the workspace, which the call's one packing launch makes.
 struct Rows {
     const void *p;
     int64_t ld;
 };
-static int ffn_rows(int dtype, const void *p, int64_t ld, int64_t rows, int64_t width, char *copy, int64_t ld_copy,
-                    hipStream_t stream, Rows *out) {
-    if (dtype == ANN_F32 || ffn_direct(p, ld, width)) {
-        *out = {p, ld};
-        return ANN_OK;
-    }
-    *out = {copy, ld_copy};
-    return launch_pad_rows(p, ld, rows, width, copy, ld_copy, stream);
+static Rows ffn_rows(int dtype, const void *p, int64_t ld, int64_t rows, int64_t width, char *copy, int64_t ld_copy, PadRows *pads) {
+    if (dtype == ANN_F32 || ffn_direct(p, ld, width)) return {p, ld};
+    pads->item[pads->n++] = {p, ld, rows, width, copy, ld_copy};
+    return {copy, ld_copy};
 }
 
 static bool ffn_sizes(int64_t M, int32_t D, int32_t F, int32_t O, int32_t dtype) {
@@ -245,14 +243,13 @@ int ann_gated_ffn(const void *x_dev, int64_t ld_x, const void *w_in_dev, const v
     hipStream_t s = (hipStream_t)stream;
     const bool few_in = M <= ffn_few(dtype, FFN_GATE), few_out = M <= ffn_few(dtype, FFN_STORE);
     Rows x = {x_dev, ld_x}, w_in = {w_in_dev, d_in}, w_out = {w_out_dev, d_hidden};
-    rc = ANN_OK;
+    PadRows pads = {};
     if (!few_in) {
-        rc = ffn_rows(dtype, x_dev, ld_x, M, d_in, ws + plan.x, plan.D8, s, &x);
-        if (rc == ANN_OK)
-            rc = ffn_rows(dtype, w_in_dev, d_in, (int64_t)2 * d_hidden, d_in, ws + plan.w_in, plan.D8, s, &w_in);
+        x = ffn_rows(dtype, x_dev, ld_x, M, d_in, ws + plan.x, plan.D8, &pads);
+        w_in = ffn_rows(dtype, w_in_dev, d_in, (int64_t)2 * d_hidden, d_in, ws + plan.w_in, plan.D8, &pads);
     }
-    if (!few_out && rc == ANN_OK)
-        rc = ffn_rows(dtype, w_out_dev, d_hidden, d_out, d_hidden, ws + plan.w_out, plan.F8, s, &w_out);
+    if (!few_out) w_out = ffn_rows(dtype, w_out_dev, d_hidden, d_out, d_hidden, ws + plan.w_out, plan.F8, &pads);
+    rc = launch_pad_rows(pads, s);
     if (rc != ANN_OK) return rc;
     FfnProduct p = {};
     p.kind = dtype, p.epi = FFN_GATE, p.a_rows = true, p.b_rows = true;
@@ -309,12 +306,17 @@ int ann_gated_ffn_backward(const void *dout_dev, int64_t ld_dout, const void *x_
     char *ws = (char *)workspace_dev;
     float *part = (float *)(ws + plan.part);
     void *dpre = ws + plan.dpre, *h = ws + plan.h;
-    Rows dout = {dout_dev, ld_dout}, x = {x_dev, ld_x}, w_in = {w_in_dev, d_in}, w_out = {w_out_dev, d_hidden};
     const bool hidden = dx_dev || dw_in_dev || db_in_dev;  // the gradient of gate and up is wanted
-    rc = ANN_OK;
+    Rows dout = {dout_dev, ld_dout}, x = {x_dev, ld_x}, w_in = {w_in_dev, d_in}, w_out = {w_out_dev, d_hidden};
+    PadRows pads = {};
     if (hidden || dw_out_dev) {
-        rc = ffn_rows(dtype, dout_dev, ld_dout, M, d_out, ws + plan.dout, plan.O8, s, &dout);
-        if (rc == ANN_OK) rc = ffn_rows(dtype, w_out_dev, d_hidden, d_out, d_hidden, ws + plan.w_out, plan.F8, s, &w_out);
+        dout = ffn_rows(dtype, dout_dev, ld_dout, M, d_out, ws + plan.dout, plan.O8, &pads);
+        w_out = ffn_rows(dtype, w_out_dev, d_hidden, d_out, d_hidden, ws + plan.w_out, plan.F8, &pads);
+    }
+    if (dx_dev) w_in = ffn_rows(dtype, w_in_dev, d_in, (int64_t)2 * d_hidden, d_in, ws + plan.w_in, plan.D8, &pads);
+    if (dw_in_dev) x = ffn_rows(dtype, x_dev, ld_x, M, d_in, ws + plan.x, plan.D8, &pads);
+    rc = launch_pad_rows(pads, s);
+    if (rc == ANN_OK && (hidden || dw_out_dev)) {
         FfnProduct p = {};
         p.kind = dtype, p.epi = FFN_GRAD, p.a_rows = true, p.b_rows = false;
         p.args.A = dout.p, p.args.lda = dout.ld, p.args.B = w_out.p, p.args.ldb = w_out.ld;
@@ -322,25 +324,23 @@ int ann_gated_ffn_backward(const void *dout_dev, int64_t ld_dout, const void *x_
         p.args.C = dpre, p.args.ldc = plan.ld_pre, p.args.up = d_hidden, p.args.pad = dtype != ANN_F32;
         p.args.h = dw_out_dev ? h : nullptr, p.args.ldh = plan.F8;
         p.args.pre = const_cast<float *>(pre_dev), p.args.act = act;
-        if (rc == ANN_OK) rc = launch_ffn_product(p, part, s);
+        rc = launch_ffn_product(p, part, s);
     }
     if (rc == ANN_OK && dx_dev) {
-        rc = ffn_rows(dtype, w_in_dev, d_in, (int64_t)2 * d_hidden, d_in, ws + plan.w_in, plan.D8, s, &w_in);
         FfnProduct p = {};
         p.kind = dtype, p.epi = FFN_STORE, p.a_rows = true, p.b_rows = false;
         p.args.A = dpre, p.args.lda = plan.ld_pre, p.args.B = w_in.p, p.args.ldb = w_in.ld;
         p.args.M = (int32_t)M, p.args.N = d_in, p.args.K = 2 * d_hidden;
         p.args.C = dx_dev, p.args.ldc = ld_dx;
-        if (rc == ANN_OK) rc = launch_ffn_product(p, part, s);
+        rc = launch_ffn_product(p, part, s);
     }
     if (rc == ANN_OK && dw_in_dev) {
-        rc = ffn_rows(dtype, x_dev, ld_x, M, d_in, ws + plan.x, plan.D8, s, &x);
         FfnProduct p = {};
         p.kind = dtype, p.epi = FFN_STORE, p.a_rows = false, p.b_rows = false;
         p.args.A = dpre, p.args.lda = plan.ld_pre, p.args.B = x.p, p.args.ldb = x.ld;
         p.args.M = 2 * d_hidden, p.args.N = d_in, p.args.K = (int32_t)M;
         p.args.C = dw_in_dev, p.args.ldc = d_in;
-        if (rc == ANN_OK) rc = launch_ffn_product(p, part, s);
+        rc = launch_ffn_product(p, part, s);
     }
     if (rc == ANN_OK && dw_out_dev) {
         FfnProduct p = {};
@@ -350,9 +350,12 @@ int ann_gated_ffn_backward(const void *dout_dev, int64_t ld_dout, const void *x_
         p.args.C = dw_out_dev, p.args.ldc = d_hidden;
         rc = launch_ffn_product(p, part, s);
     }
-    if (rc == ANN_OK && db_in_dev)
-        rc = launch_column_sum(dpre, M, (int64_t)2 * d_hidden, plan.ld_pre, dtype, db_in_dev, dtype, part, s);
-    if (rc == ANN_OK && db_out_dev) rc = launch_column_sum(dout_dev, M, d_out, ld_dout, dtype, db_out_dev, dtype, part, s);
+    if (rc == ANN_OK && (db_in_dev || db_out_dev)) {
+        ColumnSums sums = {};
+        if (db_in_dev) sums.item[sums.n++] = {dpre, (int64_t)2 * d_hidden, plan.ld_pre, db_in_dev, nullptr};
+        if (db_out_dev) sums.item[sums.n++] = {dout_dev, d_out, ld_dout, db_out_dev, nullptr};
+        rc = launch_column_sums(sums, M, dtype, part, s);
+    }
     return rc;
 }
 

@@ -81,19 +81,30 @@ ln_forward_kernel(const typename ElemOf<KIND>::type *x, int64_t ld_x,
             if (beta) bt[j] = load_part(beta + c, left[j]);
         }
     }
-    for (int64_t r0 = (int64_t)blockIdx.x * teams; r0 < M; r0 += (int64_t)gridDim.x * teams) {
+    // the next row is on its way while one is worked on
+    const int64_t step = (int64_t)gridDim.x * teams, mine = LANES ? 0 : threadIdx.x / lanes;
+    P next[NV];
+    auto fetch = [&](int64_t row) {
+        if (row >= M) return;
+#pragma unroll
+        for (int j = 0; j < NV; ++j)
+            if (left[j] > 0) next[j] = load_part(x + row * ld_x + (j * team_size + lane) * V, left[j]);
+    };
+    fetch((int64_t)blockIdx.x * teams + mine);
+    for (int64_t r0 = (int64_t)blockIdx.x * teams; r0 < M; r0 += step) {
         // teams behind the last row follow along: the lanes of a wave sum together
-        const int64_t row = r0 + (LANES ? 0 : threadIdx.x / lanes);
+        const int64_t row = r0 + mine;
         const bool on = row < M;
         P raw[NV];
         float sum[1] = {0.f};
 #pragma unroll
+        for (int j = 0; j < NV; ++j) raw[j] = next[j];
+        fetch(row + step);
+#pragma unroll
         for (int j = 0; j < NV; ++j)
-            if (on && left[j] > 0) {
-                raw[j] = load_part(x + row * ld_x + (j * team_size + lane) * V, left[j]);
+            if (on && left[j] > 0)
 #pragma unroll
                 for (int i = 0; i < V; ++i) sum[0] += (float)raw[j][i];
-            }
         team_sum<LANES, 1>(sum, lanes, s);
         const float mean = sum[0] * inv_d;
         float sq[1] = {0.f};
@@ -198,18 +209,30 @@ ln_backward_kernel(const typename ElemOf<KIND>::type *dout, int64_t ld_dout, con
         for (int i = 0; i < V; ++i) gm[j][i] = (T)1.f, dg[j][i] = 0.f, db[j][i] = 0.f;
         if (gamma && left[j] > 0) gm[j] = load_part(gamma + c, left[j]);
     }
-    for (int64_t r0 = (int64_t)blockIdx.x * teams; r0 < M; r0 += (int64_t)gridDim.x * teams) {
-        const int64_t row = r0 + (LANES ? 0 : threadIdx.x / lanes);
+    // the next row is on its way while one is worked on
+    const int64_t step = (int64_t)gridDim.x * teams, mine = LANES ? 0 : threadIdx.x / lanes;
+    P xn[NV], yn[NV];
+    float mean_n = 0.f, rstd_n = 0.f;
+    auto fetch = [&](int64_t row) {
+        if (row >= M) return;
+#pragma unroll
+        for (int j = 0; j < NV; ++j)
+            if (left[j] > 0) {
+                const int c = (j * team_size + lane) * V;
+                xn[j] = load_part(x + row * ld_x + c, left[j]);
+                yn[j] = load_part(dout + row * ld_dout + c, left[j]);
+            }
+        mean_n = mean_in[row], rstd_n = rstd_in[row];
+    };
+    fetch((int64_t)blockIdx.x * teams + mine);
+    for (int64_t r0 = (int64_t)blockIdx.x * teams; r0 < M; r0 += step) {
+        const int64_t row = r0 + mine;
         const bool on = row < M;
         P xr[NV], yr[NV];
 #pragma unroll
-        for (int j = 0; j < NV; ++j)
-            if (on && left[j] > 0) {
-                const int c = (j * team_size + lane) * V;
-                xr[j] = load_part(x + row * ld_x + c, left[j]);
-                yr[j] = load_part(dout + row * ld_dout + c, left[j]);
-            }
-        const float mean = on ? mean_in[row] : 0.f, rstd = on ? rstd_in[row] : 0.f;
+        for (int j = 0; j < NV; ++j) xr[j] = xn[j], yr[j] = yn[j];
+        const float mean = mean_n, rstd = rstd_n;
+        fetch(row + step);
         float sums[2] = {0.f, 0.f};
 #pragma unroll
         for (int j = 0; j < NV; ++j)
@@ -384,20 +407,20 @@ static RowPlan row_plan(int64_t d, int dtype) {
     return {1024, 0, 0};
 }
 
-// Workgroups of the gradient, each of which writes 2 d sums: 16 waves a compute unit, no more than there are rows.
-static int64_t backward_groups(int64_t M, const RowPlan &p) {
-    const int64_t teams = p.lanes ? 256 / p.lanes : 1, groups = (M + teams - 1) / teams, most = p.threads == 1024 ? 256 : 512;
-    return groups < most ? groups : most;
+// Workgroups: at most `most`, each with the same number of rounds or one less.
+static int64_t row_groups(int64_t M, const RowPlan &p, int64_t most) {
+    const int64_t teams = p.lanes ? 256 / p.lanes : 1, groups = (M + teams - 1) / teams, rounds = (groups + most - 1) / most;
+    return (groups + rounds - 1) / rounds;
 }
+// Of the gradient, where each workgroup writes 2 d sums: two of 256 threads a compute unit.
+static int64_t backward_groups(int64_t M, const RowPlan &p) { return row_groups(M, p, p.threads == 1024 ? 256 : 512); }
 
 template <int KIND>
 static int launch_forward(const void *x, int64_t ld_x, const void *gamma, const void *beta, void *out, int64_t ld_out,
                           float *mean, float *rstd, int64_t M, int d, float eps, hipStream_t stream) {
     using T = typename ElemOf<KIND>::type;
     const RowPlan p = row_plan(d, KIND);
-    const int64_t teams = p.lanes ? 256 / p.lanes : 1, groups = (M + teams - 1) / teams;
-    const int64_t most = p.threads == 1024 ? 512 : 2048;
-    const dim3 grid((unsigned)(groups < most ? groups : most));
+    const dim3 grid((unsigned)row_groups(M, p, p.threads == 1024 ? 512 : 2048));
     if (p.nv == 0) {
         hipLaunchKernelGGL(ln_forward_any_kernel<KIND>, grid, dim3(1024), 0, stream, (const T *)x, ld_x, (const T *)gamma,
                            (const T *)beta, (T *)out, ld_out, mean, rstd, M, d, eps);

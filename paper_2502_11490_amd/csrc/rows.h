@@ -53,15 +53,23 @@ template <typename T> __device__ __forceinline__ void store_floats(T *p, int lef
 inline bool row_dtype(int32_t dtype) { return dtype == ANN_F32 || dtype == ANN_BF16 || dtype == ANN_F16; }
 inline size_t elem_bytes(int32_t dtype) { return dtype == ANN_F32 ? 4 : 2; }
 
-// rows.hip: out[c] = sum over P of part[p][c], in the order of p, rounded to KIND once; part [P][n] fp32
-int launch_sum_parts(const float *part, int64_t P, int64_t n, void *out, int dtype, hipStream_t stream);
-// rows.hip: the same for part [P][2][n] and two results, either of which may be null
+// rows.hip: first[c] (c < n) and second[c - n] = sum over P of part[p][c], in the order of p, rounded once to dtype; part
+// [P][2 n] fp32, either result may be null
 int launch_sum_two(const float *part, int64_t P, int64_t n, void *first, void *second, int dtype, hipStream_t stream);
 // rows.hip: n elements of zeros
 int launch_zero(void *out, int64_t n, int dtype, hipStream_t stream);
-// rows.hip: column sums of a [M][n] array of `dtype` (row stride ld), deterministic; part: column_sum_parts(M, n) * n floats
+// rows.hip: column sums of one or two [M][n] arrays of `dtype`, deterministic; part: column_sum_parts(M, all columns) *
+// all columns floats
+struct ColumnSums {
+    struct Item {
+        const void *in;
+        int64_t n, ld;
+        void *out;
+        float *part;
+    } item[2];
+    int n;
+};
 int64_t column_sum_parts(int64_t M, int64_t n);
-int launch_column_sum(const void *in, int64_t M, int64_t n, int64_t ld, int in_dtype, void *out, int dtype, float *part,
-                      hipStream_t stream);
+int launch_column_sums(const ColumnSums &sums, int64_t M, int dtype, float *part, hipStream_t stream);
 
 }  // namespace gmpgr

@@ -4,15 +4,14 @@
 
 namespace gmpgr {
 
-// part [P][width], the first n columns of which go to `first`, the others to `second`.  One thread a column and slice of
-// parts; the 8 slices of a workgroup are joined in order.
+// Adds the parts of 32 columns, one thread a column and eighth of the parts; the eighths are joined in order.
 template <int KIND>
-__global__ void __launch_bounds__(256)
-sum_parts_kernel(const float *__restrict__ part, int64_t P, int64_t width, int64_t n,
-                 typename ElemOf<KIND>::type *__restrict__ first, typename ElemOf<KIND>::type *__restrict__ second) {
+__device__ __forceinline__ void sum_columns(const float *__restrict__ part, int64_t P, int64_t width, int64_t first_col,
+                                            int64_t n, typename ElemOf<KIND>::type *first,
+                                            typename ElemOf<KIND>::type *second) {
     __shared__ float s[8][32];
     const int c = threadIdx.x & 31, y = threadIdx.x >> 5;
-    const int64_t col = (int64_t)blockIdx.x * 32 + c;
+    const int64_t col = first_col + c;
     float acc = 0.f;
     if (col < width) {
         const int64_t p0 = P * y / 8, p1 = P * (y + 1) / 8;
@@ -29,25 +28,23 @@ sum_parts_kernel(const float *__restrict__ part, int64_t P, int64_t width, int64
     }
 }
 
-static int launch_sum(const float *part, int64_t P, int64_t width, int64_t n, void *first, void *second, int dtype,
-                      hipStream_t stream) {
-    const dim3 grid((unsigned)((width + 31) / 32));
-    if (dtype == ANN_F32)
-        hipLaunchKernelGGL(sum_parts_kernel<ANN_F32>, grid, dim3(256), 0, stream, part, P, width, n, (float *)first, (float *)second);
-    else if (dtype == ANN_BF16)
-        hipLaunchKernelGGL(sum_parts_kernel<ANN_BF16>, grid, dim3(256), 0, stream, part, P, width, n, (__bf16 *)first, (__bf16 *)second);
-    else
-        hipLaunchKernelGGL(sum_parts_kernel<ANN_F16>, grid, dim3(256), 0, stream, part, P, width, n, (_Float16 *)first, (_Float16 *)second);
-    ANN_HIP_TRY(hipGetLastError());
-    return ANN_OK;
-}
-
-int launch_sum_parts(const float *part, int64_t P, int64_t n, void *out, int dtype, hipStream_t stream) {
-    return launch_sum(part, P, n, n, out, nullptr, dtype, stream);
+template <int KIND>
+__global__ void __launch_bounds__(256)
+sum_two_kernel(const float *__restrict__ part, int64_t P, int64_t n, typename ElemOf<KIND>::type *first,
+               typename ElemOf<KIND>::type *second) {
+    sum_columns<KIND>(part, P, 2 * n, (int64_t)blockIdx.x * 32, n, first, second);
 }
 
 int launch_sum_two(const float *part, int64_t P, int64_t n, void *first, void *second, int dtype, hipStream_t stream) {
-    return launch_sum(part, P, 2 * n, n, first, second, dtype, stream);
+    const dim3 grid((unsigned)((2 * n + 31) / 32));
+    if (dtype == ANN_F32)
+        hipLaunchKernelGGL(sum_two_kernel<ANN_F32>, grid, dim3(256), 0, stream, part, P, n, (float *)first, (float *)second);
+    else if (dtype == ANN_BF16)
+        hipLaunchKernelGGL(sum_two_kernel<ANN_BF16>, grid, dim3(256), 0, stream, part, P, n, (__bf16 *)first, (__bf16 *)second);
+    else
+        hipLaunchKernelGGL(sum_two_kernel<ANN_F16>, grid, dim3(256), 0, stream, part, P, n, (_Float16 *)first, (_Float16 *)second);
+    ANN_HIP_TRY(hipGetLastError());
+    return ANN_OK;
 }
 
 __global__ void __launch_bounds__(256) zero_kernel(uint16_t *out, int64_t n) {
@@ -63,24 +60,25 @@ int launch_zero(void *out, int64_t n, int dtype, hipStream_t stream) {
     return ANN_OK;
 }
 
-// A workgroup sums a slice of rows of 64 16-byte pieces of columns: 4 waves take every fourth row, joined in LDS.
-template <int KIND>
-__global__ void __launch_bounds__(256)
-column_sum_kernel(const typename ElemOf<KIND>::type *__restrict__ in, int64_t M, int64_t n, int64_t ld,
-                  float *__restrict__ part) {
+// A workgroup sums a slice of rows of 64 16-byte pieces of columns of one of the arrays: 4 waves take every fourth row, joined
+// in LDS.
+template <int KIND> __global__ void __launch_bounds__(256) column_sums_kernel(ColumnSums sums, int64_t M, int first_groups) {
     using T = typename ElemOf<KIND>::type;
     constexpr int V = VEC<T>;
     __shared__ float s[3][64 * V];
+    const bool second = (int)blockIdx.x >= first_groups;
+    const ColumnSums::Item &a = sums.item[second];
+    const T *in = (const T *)a.in;
     const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-    const int64_t col = ((int64_t)blockIdx.x * 64 + lane) * V;
-    const int left = n - col < V ? (int)(n - col) : V;
+    const int64_t col = ((int64_t)(blockIdx.x - (second ? first_groups : 0)) * 64 + lane) * V;
+    const int left = a.n - col < V ? (a.n > col ? (int)(a.n - col) : 0) : V;
     const int64_t r0 = M * blockIdx.y / gridDim.y, r1 = M * (blockIdx.y + 1) / gridDim.y;
     float acc[V] = {};
     if (left > 0)
 #pragma unroll 4
         for (int64_t r = r0 + w; r < r1; r += 4) {
             float v[V];
-            load_floats(in + r * ld + col, left, v);
+            load_floats(in + r * a.ld + col, left, v);
 #pragma unroll
             for (int i = 0; i < V; ++i) acc[i] += v[i];
         }
@@ -92,60 +90,80 @@ column_sum_kernel(const typename ElemOf<KIND>::type *__restrict__ in, int64_t M,
 #pragma unroll
         for (int i = 0; i < V; ++i)
             if (i < left)
-                part[(int64_t)blockIdx.y * n + col + i] = ((acc[i] + s[0][i * 64 + lane]) + s[1][i * 64 + lane]) + s[2][i * 64 + lane];
+                a.part[(int64_t)blockIdx.y * a.n + col + i] = ((acc[i] + s[0][i * 64 + lane]) + s[1][i * 64 + lane]) + s[2][i * 64 + lane];
     }
 }
 
-// Slices of rows: enough workgroups for two a compute unit, at least 32 rows each.
+template <int KIND> __global__ void __launch_bounds__(256) sum_column_parts_kernel(ColumnSums sums, int64_t P, int first_groups) {
+    const bool second = (int)blockIdx.x >= first_groups;
+    const ColumnSums::Item &a = sums.item[second];
+    sum_columns<KIND>(a.part, P, a.n, (int64_t)(blockIdx.x - (second ? first_groups : 0)) * 32, a.n,
+                      (typename ElemOf<KIND>::type *)a.out, nullptr);
+}
+
+// Slices of rows: enough workgroups for four a compute unit, at least 16 rows each.
 int64_t column_sum_parts(int64_t M, int64_t n) {
     const int64_t across = (n + 511) / 512;
-    int64_t p = 512 / (across < 512 ? across : 512);
-    if (p > (M + 31) / 32) p = (M + 31) / 32;
+    int64_t p = 1024 / (across < 1024 ? across : 1024);
+    if (p > (M + 15) / 16) p = (M + 15) / 16;
     return p < 1 ? 1 : p;
 }
 
-int launch_column_sum(const void *in, int64_t M, int64_t n, int64_t ld, int in_dtype, void *out, int dtype, float *part,
-                      hipStream_t stream) {
-    const int64_t P = column_sum_parts(M, n);
-    const int V = (int)(16 / elem_bytes(in_dtype));
-    const dim3 grid((unsigned)((n + 64 * V - 1) / (64 * V)), (unsigned)P);
-    if (in_dtype == ANN_F32)
-        hipLaunchKernelGGL(column_sum_kernel<ANN_F32>, grid, dim3(256), 0, stream, (const float *)in, M, n, ld, part);
-    else if (in_dtype == ANN_BF16)
-        hipLaunchKernelGGL(column_sum_kernel<ANN_BF16>, grid, dim3(256), 0, stream, (const __bf16 *)in, M, n, ld, part);
-    else
-        hipLaunchKernelGGL(column_sum_kernel<ANN_F16>, grid, dim3(256), 0, stream, (const _Float16 *)in, M, n, ld, part);
+template <int KIND> static int launch_column_sums_of(const ColumnSums &sums, int64_t M, int64_t P, hipStream_t stream) {
+    auto groups = [](const ColumnSums::Item &a, int64_t cols) { return (a.n + cols - 1) / cols; };
+    const int64_t cols = 64 * VEC<typename ElemOf<KIND>::type>;
+    const int64_t first = groups(sums.item[0], cols), all = first + (sums.n > 1 ? groups(sums.item[1], cols) : 0);
+    hipLaunchKernelGGL(column_sums_kernel<KIND>, dim3((unsigned)all, (unsigned)P), dim3(256), 0, stream, sums, M, (int)first);
     ANN_HIP_TRY(hipGetLastError());
-    return launch_sum_parts(part, P, n, out, dtype, stream);
+    const int64_t first32 = groups(sums.item[0], 32), all32 = first32 + (sums.n > 1 ? groups(sums.item[1], 32) : 0);
+    hipLaunchKernelGGL(sum_column_parts_kernel<KIND>, dim3((unsigned)all32), dim3(256), 0, stream, sums, P, (int)first32);
+    ANN_HIP_TRY(hipGetLastError());
+    return ANN_OK;
 }
 
-// 8 elements a thread.
-__global__ void __launch_bounds__(256)
-pad_rows_kernel(const uint16_t *__restrict__ in, int64_t ld_in, int64_t rows, int64_t width, uint16_t *__restrict__ out, int64_t ld_out) {
+int launch_column_sums(const ColumnSums &given, int64_t M, int dtype, float *part, hipStream_t stream) {
+    ColumnSums sums = given;
+    const int64_t P = column_sum_parts(M, sums.item[0].n + (sums.n > 1 ? sums.item[1].n : 0));
+    sums.item[0].part = part;
+    if (sums.n > 1) sums.item[1].part = part + P * sums.item[0].n;
+    if (dtype == ANN_F32) return launch_column_sums_of<ANN_F32>(sums, M, P, stream);
+    if (dtype == ANN_BF16) return launch_column_sums_of<ANN_BF16>(sums, M, P, stream);
+    return launch_column_sums_of<ANN_F16>(sums, M, P, stream);
+}
+
+// 8 elements a thread, one array after the other.
+__global__ void __launch_bounds__(256) pad_rows_kernel(PadRows p) {
     typedef uint16_t u16x8 __attribute__((ext_vector_type(8)));
     struct __attribute__((packed, aligned(2))) Pack {
         u16x8 v;
     };
-    const int64_t across = ld_out / 8, total = rows * across;
-    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
-        const int64_t r = i / across, c = (i - r * across) * 8, left = width - c;
-        const uint16_t *p = in + r * ld_in + c;
-        u16x8 v = {0, 0, 0, 0, 0, 0, 0, 0};
-        if (left >= 8) {
-            v = reinterpret_cast<const Pack *>(p)->v;
-        } else {
+    for (int a = 0; a < p.n; ++a) {
+        const PadRows::Item &t = p.item[a];
+        const int64_t across = t.ld_out / 8, total = t.rows * across;
+        for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
+            const int64_t r = i / across, c = (i - r * across) * 8, left = t.width - c;
+            const uint16_t *from = (const uint16_t *)t.in + r * t.ld_in + c;
+            u16x8 v = {0, 0, 0, 0, 0, 0, 0, 0};
+            if (left >= 8) {
+                v = reinterpret_cast<const Pack *>(from)->v;
+            } else {
 #pragma unroll
-            for (int e = 0; e < 8; ++e)
-                if (e < left) v[e] = p[e];
+                for (int e = 0; e < 8; ++e)
+                    if (e < left) v[e] = from[e];
+            }
+            *(u16x8 *)((uint16_t *)t.out + r * t.ld_out + c) = v;
         }
-        *(u16x8 *)(out + r * ld_out + c) = v;
     }
 }
 
-int launch_pad_rows(const void *in, int64_t ld_in, int64_t rows, int64_t width, void *out, int64_t ld_out, hipStream_t stream) {
-    const int64_t groups = (rows * (ld_out / 8) + 255) / 256;
-    hipLaunchKernelGGL(pad_rows_kernel, dim3((unsigned)(groups < 8192 ? groups : 8192)), dim3(256), 0, stream,
-                       (const uint16_t *)in, ld_in, rows, width, (uint16_t *)out, ld_out);
+int launch_pad_rows(const PadRows &p, hipStream_t stream) {
+    if (p.n == 0) return ANN_OK;
+    int64_t groups = 1;
+    for (int a = 0; a < p.n; ++a) {
+        const int64_t g = (p.item[a].rows * (p.item[a].ld_out / 8) + 255) / 256;
+        if (g > groups) groups = g;
+    }
+    hipLaunchKernelGGL(pad_rows_kernel, dim3((unsigned)(groups < 4096 ? groups : 4096)), dim3(256), 0, stream, p);
     ANN_HIP_TRY(hipGetLastError());
     return ANN_OK;
 }
