@@ -469,8 +469,8 @@ int ann_dropout(const void *x_dev, const void *residual_dev, void *out_dev, int6
  *   act       : ANN_SILU z * sigmoid(z), ANN_GELU z * Phi(z) (the normal distribution function, not its tanh form),
  *               ANN_SIGMOID, ANN_RELU
  *   pre_dev   [M][2 * d_hidden] fp32          : gate and up before the activation, written for the gradient; NULL where none is taken
- * Products are accumulated in fp32.  In the 16-bit types h is rounded to the type, as the operand of the second product;
- * gate and up are not rounded.  fp16 overflows where the formula's h or out do.
+ * Products are accumulated in fp32.  In the 16-bit types h is rounded to the type, as the operand of the second product
+ * (with up to 8 rows it keeps twice the type's bits); gate and up are not rounded.  fp16 overflows where the formula's h or out do.
  * M >= 0 (0: nothing is done), M < 2^31; every width 1 .. 2^20.
  * workspace_dev: ann_gated_ffn_workspace_bytes with the same sizes (0 on invalid ones).
  */
@@ -485,8 +485,8 @@ int ann_gated_ffn(const void *x_dev, int64_t ld_x, const void *w_in_dev, const v
  * Its gradient, with (gate, up) = pre as the forward call wrote it, h = act(gate) * up:
  *     dh = dout w_out, dgate = dh * up * act'(gate), dup = dh * act(gate), dx = [dgate | dup] w_in,
  *     dw_in = [dgate | dup]^T x, dw_out = dout^T h, db_in = column sums of [dgate | dup], db_out = column sums of dout.
- * In the 16-bit types dgate, dup and h are rounded to the type, as operands of the products (and db_in sums the rounded
- * values); nothing else is rounded before the results.  ANN_RELU has slope 0 at 0.
+ * In the 16-bit types dgate, dup and h are rounded to the type, as operands of the products; nothing else is rounded
+ * before the results (db_in sums dgate and dup before their rounding).  ANN_RELU has slope 0 at 0.
  * dout_dev [M][d_out]; dx_dev [M][d_in] must not overlap dout_dev or x_dev; dx_dev, dw_in_dev, db_in_dev, dw_out_dev,
  * db_out_dev have the shapes of what they are gradients of, NULL = not wanted.  With M = 0 the parameters' gradients are zeroed.
  * workspace_dev: ann_gated_ffn_backward_workspace_bytes with the same sizes (0 on invalid ones).

@@ -15,6 +15,7 @@ enum FfnEpi {
 // C [M][N] = sum over k < K of A(m, k) B(n, k); where an operand's k are contiguous it is [rows][ld], else [k][ld].
 struct FfnArgs {
     const void *A, *B;
+    const void *A_rest;   // few rows: what A's rounding left over, added to it in the products (null = nothing)
     int64_t lda, ldb;
     int32_t M, N, K;      // FFN_GATE: N = d_hidden, B has rows 0 .. N - 1 for the gate, up .. up + N - 1 for up
     int32_t up;           // FFN_GRAD: C has the gate's columns from 0 and up's from `up` on
@@ -22,9 +23,10 @@ struct FfnArgs {
     int64_t ldc;
     const void *bias;     // [N], FFN_GATE: [2 N]; null = none
     float *pre;           // [M][2 N]: FFN_GATE writes it (null = not), FFN_GRAD reads it
-    void *h;              // [M][ldh], FFN_GRAD writes it (null = not)
+    void *h;              // [M][ldh], FFN_GRAD writes h; FFN_GATE what C's rounding leaves over (null = not)
     int64_t ldh;
     bool pad;             // C's rows are padded (to 8 columns) for the next product: zeros go behind the last column
+    float *cols;          // [row blocks][2 N], FFN_GRAD in 16 bits writes its column sums over blocks of rows (null = not)
     int32_t act;
     // sums over slices of k: slice s writes part[s][M][N or 2 N] in place of the epilogue
     float *part;
@@ -124,10 +126,10 @@ struct FfnFalse {
 };
 
 // W consecutive columns from n on of row m (the caller has m < M, n < N); `up` for FFN_GATE only.  INSIDE: all of the
-// tile's columns are inside, so that nothing is padded either.
+// tile's columns are inside, so that nothing is padded either.  dgate, dup: what FFN_GRAD writes, before its rounding.
 template <int KIND, int EPI, int W, bool INSIDE = false>
 __device__ __forceinline__ void ffn_epilogue(const FfnArgs &p, int64_t m, int n, const float *sum, const float *up,
-                                             const FfnRow<W> &r) {
+                                             const FfnRow<W> &r, float *dgate = nullptr, float *dup = nullptr) {
     using T = typename ElemOf<KIND>::type;
     const int left = INSIDE ? W : p.N - n;
     T *C = (T *)p.C + m * p.ldc + n;
@@ -160,6 +162,14 @@ __device__ __forceinline__ void ffn_epilogue(const FfnArgs &p, int64_t m, int n,
 #pragma unroll
         for (int i = 0; i < W; ++i) v[i] *= u[i];
         store_cols<W>(C, left, v);
+        if (p.h) {
+#pragma unroll
+            for (int i = 0; i < W; ++i) {
+                const float kept = (float)(T)v[i];
+                v[i] = __builtin_isinf(kept) ? 0.f : v[i] - kept;
+            }
+            store_cols<W>((T *)p.h + m * p.ldh + n, left, v);
+        }
         if (!INSIDE && p.pad && left <= W)
             for (int64_t i = p.N; i < p.ldc; ++i) ((T *)p.C + m * p.ldc)[i] = (T)0.f;
     } else {
@@ -170,6 +180,7 @@ __device__ __forceinline__ void ffn_epilogue(const FfnArgs &p, int64_t m, int n,
             v[i] = sum[i] * r.up[i] * slope[i];
             w[i] = sum[i] * a[i];
             a[i] *= r.up[i];
+            if (dgate) dgate[i] = v[i], dup[i] = w[i];
         }
         store_cols<W>(C, left, v);
         store_cols<W>(C + p.up, left, w);
@@ -210,6 +221,8 @@ struct FfnCut {
     int rows, cols, splits;
 };
 FfnCut ffn_cut(int kind, int64_t M, int64_t N, int64_t K, int epi);
+// Row blocks of FfnArgs::cols: two a tile.
+inline int64_t ffn_col_blocks(int64_t M, int tile) { return (M + tile - 1) / tile * 2; }
 size_t ffn_part_floats(int kind, int64_t M, int64_t N, int64_t K, int epi);  // what launch_ffn_product needs as `part`
 int launch_ffn_product(const FfnProduct &p, float *part, hipStream_t stream);
 
@@ -218,9 +231,9 @@ int launch_ffn32(const FfnProduct &p, int cols, hipStream_t stream);            
 
 // ffn_few.hip: the same for few rows, both operands' k contiguous, any alignment; FFN_STORE and FFN_GATE, no slices.
 // Up to how many rows that is the faster kernel: with N = 8192 gate columns and K = 2048 in bf16 16 us against 22 for 32
-// rows and 21 against 22 for 64; with N = 2048 and K = 8192 8.5 us against 16 for one row, 16.5 against 16 for 16 and 30
-// against 16 for 32 (too few workgroups, that read x over and over); in fp32 34 against 32 and 68 against 21 for 64.
-constexpr int ffn_few(int kind, int epi) { return epi == FFN_GATE && kind != ANN_F32 ? 64 : 16; }
+// rows and 21 against 22 for 64; with N = 2048 and K = 8192 (h in two parts) 10 us against 16 for one row, 24 against 16
+// for 16 (too few workgroups, that read x over and over); in fp32 34 against 32 and 68 against 21 for 64.
+constexpr int ffn_few(int kind, int epi) { return kind == ANN_F32 ? 16 : epi == FFN_GATE ? 64 : 8; }
 int launch_ffn_few(const FfnProduct &p, hipStream_t stream);
 
 // 16-bit operands as launch_ffn16 takes them: 16-byte aligned rows, the contiguous extent a multiple of 8, and 256 rows

@@ -6,9 +6,10 @@
 // bytes l / 16 of row l % 16, of w as of x, and the instruction's k are numbered accordingly on both sides; a line of w is
 // read whole, by 4 lanes, at whatever address it begins.  With 4 (8) rows of x at most, the instruction's 16 rows are 4
 // (8) rows in 4 (2) slices of a step: four times the workgroups, so that few columns still occupy every compute unit, and of
-// the 16 x 16 sums the blocks on the diagonal are added.  Several steps' loads are on their way together.
-// One bf16 row through 2048 -> 2 x 8192 (67 MB): 13.5 us, 5.0 TB/s; 8192 -> 2048 (34 MB): 8.5 us, 4.0 TB/s (without
-// slices 11.6 us).
+// the 16 x 16 sums the blocks on the diagonal are added.  h comes in two 16-bit parts, its rounding and what that leaves
+// over: the instructions are idle anyway, and out is then as near as from an fp32 h.  Several steps' loads are on their way together.
+// One bf16 row through 2048 -> 2 x 8192 (67 MB): 13.3 us, 5.0 TB/s; 8192 -> 2048 (34 MB): 9.7 us, 3.5 TB/s (without slices
+// 11.6 us, with h in one part 8.5 us).
 #include "ffn.h"
 
 namespace gmpgr {
@@ -51,7 +52,8 @@ template <int KIND> struct FewFrag {
     }
 };
 
-template <int KIND, int EPI, int S, int MT, int RT>
+// REST: A_rest is there.
+template <int KIND, int EPI, int S, int MT, int RT, bool REST>
 __global__ void __launch_bounds__(MT > 1 ? 512 : 1024) ffn_few_kernel(FfnArgs p) {
     using T = typename ElemOf<KIND>::type;
     using Frag = FewFrag<KIND>;
@@ -61,6 +63,7 @@ __global__ void __launch_bounds__(MT > 1 ? 512 : 1024) ffn_few_kernel(FfnArgs p)
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, waves = blockDim.x >> 6, l = lane & 15;
     const int n0 = blockIdx.x * R * RT, first = l / R * Frag::K;  // first: the lane's slice of a step
     const T *w[HALVES * RT], *x[MT];
+    const int64_t rest = REST ? (const T *)p.A_rest - (const T *)p.A : 0;
 #pragma unroll
     for (int i = 0; i < HALVES * RT; ++i) {
         const int n = n0 + i % RT * R + l % R;
@@ -74,7 +77,7 @@ __global__ void __launch_bounds__(MT > 1 ? 512 : 1024) ffn_few_kernel(FfnArgs p)
     // steps go round the waves
     const int stride = waves * S * Frag::K;
     for (int k = wave * S * Frag::K; k < p.K; k += AHEAD * stride) {
-        Frag fw[AHEAD][HALVES * RT], fx[AHEAD][MT];
+        Frag fw[AHEAD][HALVES * RT], fx[AHEAD][MT], fr[REST ? AHEAD : 1][MT];
 #pragma unroll
         for (int a = 0; a < AHEAD; ++a) {
             const int at = k + a * stride;
@@ -82,7 +85,10 @@ __global__ void __launch_bounds__(MT > 1 ? 512 : 1024) ffn_few_kernel(FfnArgs p)
 #pragma unroll
                 for (int i = 0; i < HALVES * RT; ++i) fw[a][i].load(w[i], at, first, S * Frag::K, p.K);
 #pragma unroll
-                for (int i = 0; i < MT; ++i) fx[a][i].load(x[i], at, first, S * Frag::K, p.K);
+                for (int i = 0; i < MT; ++i) {
+                    fx[a][i].load(x[i], at, first, S * Frag::K, p.K);
+                    if (REST) fr[REST ? a : 0][i].load(x[i] + rest, at, first, S * Frag::K, p.K);
+                }
             }
         }
 #pragma unroll
@@ -91,7 +97,10 @@ __global__ void __launch_bounds__(MT > 1 ? 512 : 1024) ffn_few_kernel(FfnArgs p)
 #pragma unroll
                 for (int i = 0; i < HALVES * RT; ++i)
 #pragma unroll
-                    for (int j = 0; j < MT; ++j) sum[i * MT + j] = Frag::product(fw[a][i], fx[a][j], sum[i * MT + j]);
+                    for (int j = 0; j < MT; ++j) {
+                        sum[i * MT + j] = Frag::product(fw[a][i], fx[a][j], sum[i * MT + j]);
+                        if (REST) sum[i * MT + j] = Frag::product(fw[a][i], fr[REST ? a : 0][j], sum[i * MT + j]);
+                    }
     }
 #pragma unroll
     for (int i = 0; i < TILES; ++i) joined[(wave * TILES + i) * 64 + lane] = sum[i];
@@ -117,22 +126,27 @@ __global__ void __launch_bounds__(MT > 1 ? 512 : 1024) ffn_few_kernel(FfnArgs p)
     }
 }
 
-template <int KIND, int EPI, int S, int MT, int RT> static int launch_few(const FfnArgs &a, hipStream_t stream) {
+template <int KIND, int EPI, int S, int MT, int RT, bool REST = false> static int launch_few(const FfnArgs &a, hipStream_t stream) {
     constexpr int TILES = (EPI == FFN_GATE ? 2 : 1) * RT * MT, ROWS = 16 / S * RT, STEP = FewFrag<KIND>::K * S;
     const int64_t groups = ((int64_t)a.N + ROWS - 1) / ROWS, steps = ((int64_t)a.K + STEP - 1) / STEP;
     // waves of a workgroup: 16 a compute unit in all, each with a step or more, their sums within 64 KB
     int waves = 4;
     while (waves < (MT > 1 ? 8 : 16) && groups * waves < 4096 && waves < steps && waves * 2 * TILES <= 64) waves *= 2;
-    hipLaunchKernelGGL((ffn_few_kernel<KIND, EPI, S, MT, RT>), dim3((unsigned)groups), dim3(waves * 64),
+    hipLaunchKernelGGL((ffn_few_kernel<KIND, EPI, S, MT, RT, REST>), dim3((unsigned)groups), dim3(waves * 64),
                        (size_t)waves * TILES * 1024, stream, a);
     ANN_HIP_TRY(hipGetLastError());
     return ANN_OK;
 }
 
 template <int KIND, int EPI> static int launch_few_rows(const FfnArgs &a, hipStream_t stream) {
-    if (a.M <= 4) return launch_few<KIND, EPI, 4, 1, 1>(a, stream);
-    if (a.M <= 8) return launch_few<KIND, EPI, 2, 1, 1>(a, stream);
-    if (a.M <= 16) return launch_few<KIND, EPI, 1, 1, 1>(a, stream);
+    if constexpr (EPI == FFN_STORE && KIND != ANN_F32) {
+        if (a.M <= 4) return launch_few<KIND, EPI, 4, 1, 1, true>(a, stream);
+        if (a.M <= 8) return launch_few<KIND, EPI, 2, 1, 1, true>(a, stream);
+    } else {
+        if (a.M <= 4) return launch_few<KIND, EPI, 4, 1, 1>(a, stream);
+        if (a.M <= 8) return launch_few<KIND, EPI, 2, 1, 1>(a, stream);
+        if (a.M <= 16) return launch_few<KIND, EPI, 1, 1, 1>(a, stream);
+    }
     if constexpr (ffn_few(KIND, EPI) > 16) {
         // 32 columns a workgroup, which read x half as often, where that still occupies every compute unit
         if (a.N < 32 * 256) return a.M <= 32 ? launch_few<KIND, EPI, 1, 2, 1>(a, stream) : launch_few<KIND, EPI, 1, 4, 1>(a, stream);

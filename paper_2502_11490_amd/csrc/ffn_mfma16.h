@@ -218,6 +218,7 @@ __global__ void __launch_bounds__(256, BM == 256 ? 1 : 2) ffn_mfma16_kernel(FfnA
     // What the epilogue reads of memory is on its way one batch of rows ahead.  A tile inside C asks nothing per lane: with a
     // test the compiler would wait for each load where the branches meet.
     constexpr int AHEAD = HALF / ROWS < 4 ? HALF / ROWS : 4;
+    float cols[2][8] = {};  // FFN_GRAD: sums of the lane's columns of the gate's and of up's gradient, before they are rounded
     auto finish = [&](auto inside) {
         constexpr bool INSIDE = decltype(inside)::value;
 #pragma unroll
@@ -263,7 +264,11 @@ __global__ void __launch_bounds__(256, BM == 256 ? 1 : 2) ffn_mfma16_kernel(FfnA
                             store_cols<4>(o, p.N - ne, s);
                             if (GATE) store_cols<4>(o + p.N, p.N - ne, u);
                         } else {
-                            ffn_epilogue<KIND, EPI, 4, INSIDE>(p, m, ne, s, u, row[x][e]);
+                            float dg[4] = {}, du[4] = {};
+                            ffn_epilogue<KIND, EPI, 4, INSIDE>(p, m, ne, s, u, row[x][e], EPI == FFN_GRAD ? dg : nullptr, du);
+                            if (EPI == FFN_GRAD)
+#pragma unroll
+                                for (int f = 0; f < 4; ++f) cols[0][e * 4 + f] += dg[f], cols[1][e * 4 + f] += du[f];
                         }
                     }
             }
@@ -273,6 +278,23 @@ __global__ void __launch_bounds__(256, BM == 256 ? 1 : 2) ffn_mfma16_kernel(FfnA
         finish(FfnTrue{});
     else
         finish(FfnFalse{});
+    if (EPI == FFN_GRAD && p.cols) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+#pragma unroll
+                for (int o = LANES; o < 64; o <<= 1) cols[h][e] += __shfl_xor(cols[h][e], o);
+        if (lane_row == 0)
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    const int ne = n + e * (WIDE / 2);
+                    if (ne < p.N)
+                        store_cols<4>(p.cols + ((int64_t)t.m * 2 + (wave >> 1)) * 2 * p.N + h * p.N + ne, p.N - ne, cols[h] + e * 4);
+                }
+    }
 #endif
 }
 

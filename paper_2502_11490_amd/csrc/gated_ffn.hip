@@ -64,14 +64,15 @@ FfnCut ffn_cut(int kind, int64_t M, int64_t N, int64_t K, int epi) {
         FfnTileCost c = kind == ANN_F32 ? FFN_TILES32[i] : FFN_TILES16[i];
         if (c.rows == 64 && epi == FFN_GATE) c.rows = 128, c.a_unit = 2;  // gate and up of a column are one wave's
         const int64_t cols = epi == FFN_GATE ? c.cols / 2 : c.cols, tiles = ((M + c.rows - 1) / c.rows) * ((N + cols - 1) / cols);
-        for (int s = 1; s <= 16 && (s == 1 || s <= K / 256); s += s < 4 ? 1 : 2) {
+        // FFN_GRAD is not cut along k: its column sums are its tiles'
+        for (int s = 1; s <= 16 && (s == 1 || (s <= K / 256 && epi != FFN_GRAD)); s += s < 4 ? 1 : 2) {
             const int64_t slots = 256 * c.a_unit, groups = tiles * s, rounds = groups / slots, rest = groups % slots;
             const double steps = (double)((K + 64 * s - 1) / (64 * s));
             double last = (double)((rest + 255) / 256) / c.a_unit;
             if (rest > 0 && last < 1.0) last += 0.1;
             double t = ((double)rounds + last) * steps * c.step + (double)(rounds + (rest > 0)) * c.ends[s > 1 ? FFN_STORE : epi];
             if (s > 1)  // the parts come out of the caches, what the epilogue reads and writes does not
-                t += 4.0 + (double)M * (double)N * (8.0 * s * (epi == FFN_GATE ? 2 : 1) / 1.0e7 + (epi == FFN_STORE ? 0.0 : 12.0 / 4.0e6));
+                t += 4.0 + (double)M * (double)N * (8.0 * s * (epi == FFN_GATE ? 2 : 1) / 1.0e7 + (epi == FFN_GATE ? 12.0 / 4.0e6 : 0.0));
             if (least == 0.0 || t < least) least = t, best = {c.rows, c.cols, s};
         }
     }
@@ -110,9 +111,12 @@ struct Region {
 // Parts of a workspace.  x, w_in, w_out, dout: copies of operands whose rows the 16-bit kernels cannot load as they lie (an
 // odd width, stride or address); kept free for every call, because a workspace is sized before the addresses are known.
 struct FfnPlan {
-    size_t x, w_in, w_out, dout, dpre, h, part, total;
+    size_t x, w_in, w_out, dout, dpre, h, h_rest, part, cols, total;
     int64_t D8, F8, O8, ld_pre;  // row strides of the copies, of h and of dpre (fp32: as wide as the rows)
+    int64_t gate_parts, out_parts;  // cols: sums over blocks of rows, [gate_parts][2 F] for b_in's gradient, [out_parts][O]
 };
+// Few rows: h in two 16-bit parts (both products are the few rows' then).
+static bool ffn_h_rest(int64_t M, int dtype) { return dtype != ANN_F32 && M <= ffn_few(dtype, FFN_STORE); }
 static size_t most(size_t a, size_t b) { return a > b ? a : b; }
 
 static FfnPlan ffn_plan(int64_t M, int64_t D, int64_t F, int64_t O, int dtype, bool gradient) {
@@ -124,6 +128,7 @@ static FfnPlan ffn_plan(int64_t M, int64_t D, int64_t F, int64_t O, int dtype, b
     p.D8 = (D + to - 1) / to * to, p.F8 = (F + to - 1) / to * to, p.O8 = (O + to - 1) / to * to;
     p.ld_pre = (2 * F + to - 1) / to * to;
     p.h = r.take((size_t)M * p.F8 * e);
+    p.h_rest = r.take(ffn_h_rest(M, dtype) && !gradient ? (size_t)M * p.F8 * e : 0);
     const bool few_in = !gradient && M <= ffn_few(dtype, FFN_GATE), few_out = !gradient && M <= ffn_few(dtype, FFN_STORE);
     if (pack && !few_in) {
         p.x = r.take((size_t)M * p.D8 * e);
@@ -137,13 +142,16 @@ static FfnPlan ffn_plan(int64_t M, int64_t D, int64_t F, int64_t O, int dtype, b
     } else {
         if (pack) p.dout = r.take((size_t)M * p.O8 * e);
         p.dpre = r.take((size_t)M * p.ld_pre * e);
-        n = ffn_part_floats(dtype, M, F, O, FFN_GRAD);
-        n = most(n, ffn_part_floats(dtype, M, D, 2 * F, FFN_STORE));
+        n = ffn_part_floats(dtype, M, D, 2 * F, FFN_STORE);
         n = most(n, ffn_part_floats(dtype, 2 * F, D, M, FFN_STORE));
         n = most(n, ffn_part_floats(dtype, O, F, M, FFN_STORE));
-        n = most(n, (size_t)column_sum_parts(M, 2 * F + O) * (2 * F + O));
     }
     p.part = r.take(sizeof(float) * n);
+    if (gradient) {
+        p.gate_parts = pack ? ffn_col_blocks(M, ffn_cut(dtype, M, F, O, FFN_GRAD).rows) : column_sum_parts(M, 2 * F);
+        p.out_parts = column_sum_parts(M, O);
+        p.cols = r.take(sizeof(float) * ((size_t)p.gate_parts * 2 * F + (size_t)p.out_parts * O));
+    }
     p.total = r.total + 256;
     return p;
 }
@@ -257,11 +265,13 @@ int ann_gated_ffn(const void *x_dev, int64_t ld_x, const void *w_in_dev, const v
     p.args.M = (int32_t)M, p.args.N = d_hidden, p.args.K = d_in, p.args.up = d_hidden;
     p.args.C = ws + plan.h, p.args.ldc = plan.F8, p.args.pad = dtype != ANN_F32;
     p.args.bias = b_in_dev, p.args.pre = pre_dev, p.args.act = act;
+    void *rest = ffn_h_rest(M, dtype) ? ws + plan.h_rest : nullptr;
+    p.args.h = rest, p.args.ldh = plan.F8;
     rc = few_in ? launch_ffn_few(p, s) : launch_ffn_product(p, (float *)(ws + plan.part), s);
     if (rc != ANN_OK) return rc;
     FfnProduct q = {};
     q.kind = dtype, q.epi = FFN_STORE, q.a_rows = true, q.b_rows = true;
-    q.args.A = ws + plan.h, q.args.lda = plan.F8, q.args.B = w_out.p, q.args.ldb = w_out.ld;
+    q.args.A = ws + plan.h, q.args.A_rest = rest, q.args.lda = plan.F8, q.args.B = w_out.p, q.args.ldb = w_out.ld;
     q.args.M = (int32_t)M, q.args.N = d_out, q.args.K = d_hidden;
     q.args.C = out_dev, q.args.ldc = ld_out, q.args.bias = b_out_dev;
     return few_out ? launch_ffn_few(q, s) : launch_ffn_product(q, (float *)(ws + plan.part), s);
@@ -324,6 +334,7 @@ int ann_gated_ffn_backward(const void *dout_dev, int64_t ld_dout, const void *x_
         p.args.C = dpre, p.args.ldc = plan.ld_pre, p.args.up = d_hidden, p.args.pad = dtype != ANN_F32;
         p.args.h = dw_out_dev ? h : nullptr, p.args.ldh = plan.F8;
         p.args.pre = const_cast<float *>(pre_dev), p.args.act = act;
+        p.args.cols = db_in_dev && dtype != ANN_F32 ? (float *)(ws + plan.cols) : nullptr;
         rc = launch_ffn_product(p, part, s);
     }
     if (rc == ANN_OK && dx_dev) {
@@ -352,9 +363,12 @@ int ann_gated_ffn_backward(const void *dout_dev, int64_t ld_dout, const void *x_
     }
     if (rc == ANN_OK && (db_in_dev || db_out_dev)) {
         ColumnSums sums = {};
-        if (db_in_dev) sums.item[sums.n++] = {dpre, (int64_t)2 * d_hidden, plan.ld_pre, db_in_dev, nullptr};
-        if (db_out_dev) sums.item[sums.n++] = {dout_dev, d_out, ld_dout, db_out_dev, nullptr};
-        rc = launch_column_sums(sums, M, dtype, part, s);
+        float *gate = (float *)(ws + plan.cols), *out = gate + plan.gate_parts * 2 * d_hidden;
+        // in 16 bits the sums over blocks of rows are there: of the values before their rounding
+        if (db_in_dev)
+            sums.item[sums.n++] = {dtype == ANN_F32 ? dpre : nullptr, (int64_t)2 * d_hidden, plan.ld_pre, db_in_dev, gate, plan.gate_parts};
+        if (db_out_dev) sums.item[sums.n++] = {dout_dev, d_out, ld_dout, db_out_dev, out, plan.out_parts};
+        rc = launch_column_sums(sums, M, dtype, s);
     }
     return rc;
 }

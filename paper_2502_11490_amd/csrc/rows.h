@@ -58,18 +58,19 @@ inline size_t elem_bytes(int32_t dtype) { return dtype == ANN_F32 ? 4 : 2; }
 int launch_sum_two(const float *part, int64_t P, int64_t n, void *first, void *second, int dtype, hipStream_t stream);
 // rows.hip: n elements of zeros
 int launch_zero(void *out, int64_t n, int dtype, hipStream_t stream);
-// rows.hip: column sums of one or two [M][n] arrays of `dtype`, deterministic; part: column_sum_parts(M, all columns) *
-// all columns floats
+// rows.hip: column sums, deterministic, of one or two arrays: of [M][n] values of `dtype` by way of `parts` sums over slices of
+// rows in part [parts][n], or (in = null) of parts that are there already.  The results are rounded once to dtype.
 struct ColumnSums {
     struct Item {
         const void *in;
         int64_t n, ld;
         void *out;
         float *part;
+        int64_t parts;
     } item[2];
     int n;
 };
 int64_t column_sum_parts(int64_t M, int64_t n);
-int launch_column_sums(const ColumnSums &sums, int64_t M, int dtype, float *part, hipStream_t stream);
+int launch_column_sums(const ColumnSums &sums, int64_t M, int dtype, hipStream_t stream);
 
 }  // namespace gmpgr

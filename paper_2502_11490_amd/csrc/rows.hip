@@ -60,17 +60,14 @@ int launch_zero(void *out, int64_t n, int dtype, hipStream_t stream) {
     return ANN_OK;
 }
 
-// A workgroup sums a slice of rows of 64 16-byte pieces of columns of one of the arrays: 4 waves take every fourth row, joined
-// in LDS.
-template <int KIND> __global__ void __launch_bounds__(256) column_sums_kernel(ColumnSums sums, int64_t M, int first_groups) {
+// A workgroup sums a slice of rows of 64 16-byte pieces of columns: 4 waves take every fourth row, joined in LDS.
+template <int KIND> __global__ void __launch_bounds__(256) column_slices_kernel(ColumnSums::Item a, int64_t M) {
     using T = typename ElemOf<KIND>::type;
     constexpr int V = VEC<T>;
     __shared__ float s[3][64 * V];
-    const bool second = (int)blockIdx.x >= first_groups;
-    const ColumnSums::Item &a = sums.item[second];
     const T *in = (const T *)a.in;
     const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-    const int64_t col = ((int64_t)(blockIdx.x - (second ? first_groups : 0)) * 64 + lane) * V;
+    const int64_t col = ((int64_t)blockIdx.x * 64 + lane) * V;
     const int left = a.n - col < V ? (a.n > col ? (int)(a.n - col) : 0) : V;
     const int64_t r0 = M * blockIdx.y / gridDim.y, r1 = M * (blockIdx.y + 1) / gridDim.y;
     float acc[V] = {};
@@ -94,10 +91,10 @@ template <int KIND> __global__ void __launch_bounds__(256) column_sums_kernel(Co
     }
 }
 
-template <int KIND> __global__ void __launch_bounds__(256) sum_column_parts_kernel(ColumnSums sums, int64_t P, int first_groups) {
+template <int KIND> __global__ void __launch_bounds__(256) sum_column_parts_kernel(ColumnSums sums, int first_groups) {
     const bool second = (int)blockIdx.x >= first_groups;
     const ColumnSums::Item &a = sums.item[second];
-    sum_columns<KIND>(a.part, P, a.n, (int64_t)(blockIdx.x - (second ? first_groups : 0)) * 32, a.n,
+    sum_columns<KIND>(a.part, a.parts, a.n, (int64_t)(blockIdx.x - (second ? first_groups : 0)) * 32, a.n,
                       (typename ElemOf<KIND>::type *)a.out, nullptr);
 }
 
@@ -109,26 +106,25 @@ int64_t column_sum_parts(int64_t M, int64_t n) {
     return p < 1 ? 1 : p;
 }
 
-template <int KIND> static int launch_column_sums_of(const ColumnSums &sums, int64_t M, int64_t P, hipStream_t stream) {
-    auto groups = [](const ColumnSums::Item &a, int64_t cols) { return (a.n + cols - 1) / cols; };
-    const int64_t cols = 64 * VEC<typename ElemOf<KIND>::type>;
-    const int64_t first = groups(sums.item[0], cols), all = first + (sums.n > 1 ? groups(sums.item[1], cols) : 0);
-    hipLaunchKernelGGL(column_sums_kernel<KIND>, dim3((unsigned)all, (unsigned)P), dim3(256), 0, stream, sums, M, (int)first);
-    ANN_HIP_TRY(hipGetLastError());
-    const int64_t first32 = groups(sums.item[0], 32), all32 = first32 + (sums.n > 1 ? groups(sums.item[1], 32) : 0);
-    hipLaunchKernelGGL(sum_column_parts_kernel<KIND>, dim3((unsigned)all32), dim3(256), 0, stream, sums, P, (int)first32);
+template <int KIND> static int launch_column_sums_of(const ColumnSums &sums, int64_t M, hipStream_t stream) {
+    constexpr int64_t cols = 64 * VEC<typename ElemOf<KIND>::type>;
+    for (int i = 0; i < sums.n; ++i) {
+        const ColumnSums::Item &a = sums.item[i];
+        if (!a.in) continue;
+        hipLaunchKernelGGL(column_slices_kernel<KIND>, dim3((unsigned)((a.n + cols - 1) / cols), (unsigned)a.parts), dim3(256), 0,
+                           stream, a, M);
+        ANN_HIP_TRY(hipGetLastError());
+    }
+    const int64_t first = (sums.item[0].n + 31) / 32, all = first + (sums.n > 1 ? (sums.item[1].n + 31) / 32 : 0);
+    hipLaunchKernelGGL(sum_column_parts_kernel<KIND>, dim3((unsigned)all), dim3(256), 0, stream, sums, (int)first);
     ANN_HIP_TRY(hipGetLastError());
     return ANN_OK;
 }
 
-int launch_column_sums(const ColumnSums &given, int64_t M, int dtype, float *part, hipStream_t stream) {
-    ColumnSums sums = given;
-    const int64_t P = column_sum_parts(M, sums.item[0].n + (sums.n > 1 ? sums.item[1].n : 0));
-    sums.item[0].part = part;
-    if (sums.n > 1) sums.item[1].part = part + P * sums.item[0].n;
-    if (dtype == ANN_F32) return launch_column_sums_of<ANN_F32>(sums, M, P, stream);
-    if (dtype == ANN_BF16) return launch_column_sums_of<ANN_BF16>(sums, M, P, stream);
-    return launch_column_sums_of<ANN_F16>(sums, M, P, stream);
+int launch_column_sums(const ColumnSums &sums, int64_t M, int dtype, hipStream_t stream) {
+    if (dtype == ANN_F32) return launch_column_sums_of<ANN_F32>(sums, M, stream);
+    if (dtype == ANN_BF16) return launch_column_sums_of<ANN_BF16>(sums, M, stream);
+    return launch_column_sums_of<ANN_F16>(sums, M, stream);
 }
 
 // 8 elements a thread, one array after the other.
