@@ -415,13 +415,14 @@ int ann_score_pairs_noalloc(const ann_graph *g, const ann_mlp *m, const void *qu
  * fp32, in an order that depends on the sizes and the alignment only: a call repeated gives the same bits.  Row strides ld_* are
  * in elements, >= the row's width; arrays without a stride are dense.  Pointers need the alignment of their elements only, a
  * workspace 256 bytes.  Gradients are written, not added to.  Every call only enqueues kernels on `stream`, allocates
- * nothing and can be recorded into a HIP graph.  Calls that share a workspace must not overlap in time.
+ * nothing and can be recorded into a HIP graph; the arrays' device must be the current one.  Calls that share a workspace
+ * must not overlap in time.
  */
 
 /*
  * Layer norm: out[r][c] = (x[r][c] - mean_r) * rstd_r * gamma[c] + beta[c], mean_r the mean of row r,
  * rstd_r = 1 / sqrt(mean of (x[r][c] - mean_r)^2 + eps).
- *   x_dev [M][d], out_dev [M][d] : may be the same array with the same stride
+ *   x_dev [M][d], out_dev [M][d] : may be the same rows (then with the same stride), else must not overlap
  *   gamma_dev, beta_dev [d]      : NULL = ones, zeros
  *   mean_dev, rstd_dev [M] fp32  : written for the gradient; NULL where none is taken
  * M >= 0 (0: nothing is done), 1 <= d <= 2^24, eps >= 0 and finite.
@@ -434,7 +435,8 @@ int ann_layer_norm(const void *x_dev, int64_t ld_x, const void *gamma_dev, const
  * Its gradient: with g = dout * gamma and xh = (x - mean) * rstd,
  *     dx = rstd * (g - mean over the row of g - xh * mean over the row of g * xh),
  *     dgamma = sum over the rows of dout * xh, dbeta = sum over the rows of dout.
- * dout_dev [M][d]; x_dev, gamma_dev, mean_dev, rstd_dev as in the forward call.  dx_dev [M][d] may be dout_dev or x_dev;
+ * dout_dev [M][d]; x_dev, gamma_dev, mean_dev, rstd_dev as in the forward call.  dx_dev [M][d] may be dout_dev or x_dev
+ * (then with the same stride), else must not overlap them;
  * dx_dev, dgamma_dev, dbeta_dev: NULL = not wanted.  With M = 0 dgamma and dbeta are zeroed.
  * workspace_dev: ann_layer_norm_backward_workspace_bytes(M, d, dtype) bytes (0 on invalid arguments; may be NULL where
  * neither dgamma nor dbeta is wanted).
@@ -453,7 +455,8 @@ int ann_layer_norm_backward(const void *dout_dev, int64_t ld_dout, const void *x
  * element e is kept iff number e % 8 is >= t, t = round(65536 * p), and scale = 65536 / (65536 - t): p is taken to the
  * nearest 2^-16 and the mean is exact for that probability.  p = 0 keeps, p = 1 drops everything.  What a dropped element
  * holds does not matter (infinities, NaN).
- *   x_dev, residual_dev, out_dev [n] : residual_dev NULL = none; out_dev may be x_dev or residual_dev
+ *   x_dev, residual_dev, out_dev [n] : residual_dev NULL = none; out_dev may be x_dev or residual_dev, else must not
+ *                                      overlap them
  *   draw_dev                         : NULL, or one uint64 on the device that is added to `draw` when the kernel runs,
  *                                      so that the replays of a recorded call can draw anew
  */

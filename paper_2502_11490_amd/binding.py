@@ -650,7 +650,8 @@ def ann_quantize_e4m3(src: torch.Tensor, scale: float = 1.0, out: Optional[torch
 # ---- the block of a projector: y = x + dropout(ffn(layer_norm(x))) ----
 #
 # Tensors of one call lie on one device; the call goes to that device's current stream, or to `stream`, a stream of it.
-# Results and workspaces that the call makes belong to the stream it goes to.
+# Results and workspaces that the call makes belong to the stream it goes to; that its inputs are there, and stay until it
+# has read them, is the caller's to see to.  Gradients are calls of their own: these functions leave no trace in autograd.
 
 _ROW_CODE = {torch.float32: ANN_F32, torch.bfloat16: ANN_BF16, torch.float16: ANN_F16}
 

@@ -78,6 +78,12 @@ extern "C" int ann_dropout(const void *x_dev, const void *residual_dev, void *ou
         set_error("x_dev, residual_dev and out_dev must be aligned to their elements, draw_dev to 8 bytes");
         return ANN_EINVAL;
     }
+    const int64_t w = n;  // one row
+    if ((out_dev != x_dev && rows_overlap(x_dev, w, w, out_dev, w, w, 1, e)) ||
+        (residual_dev && out_dev != residual_dev && rows_overlap(residual_dev, w, w, out_dev, w, w, 1, e))) {
+        set_error("out_dev must be x_dev or residual_dev, or must not overlap them");
+        return ANN_EINVAL;
+    }
     const uint32_t threshold = (uint32_t)floor(p * 65536.0 + 0.5);
     auto fn = dtype == ANN_F32 ? launch_dropout<ANN_F32> : dtype == ANN_BF16 ? launch_dropout<ANN_BF16> : launch_dropout<ANN_F16>;
     return fn(x_dev, residual_dev, out_dev, n, threshold, seed, draw, draw_dev, (hipStream_t)stream);

@@ -1,6 +1,5 @@
 // The gated feed-forward block and its gradient: which products they are, how the products are cut, the workspace and the
-// C entry points.  The products are in ffn_mfma16.h, ffn_f32.hip and, for few rows,
-// ffn_few.hip.
+// C entry points.  The products are in ffn_mfma16.h, ffn_f32.hip and, for few rows, ffn_few.hip.
 //
 //   forward : h = act(x w_in^T) (gate, up in one product, FFN_GATE), out = h w_out^T
 //   gradient: [dgate | dup], h from dout w_out (FFN_GRAD); dx = [dgate | dup] w_in; dw_in = [dgate | dup]^T x;
@@ -17,8 +16,7 @@ template <int KIND, int EPI> __global__ void __launch_bounds__(256) ffn_finish_k
         const int64_t m = i / across;
         const int n = (int)(i - m * across) * W, left = p.N - n;
         float s[W] = {}, u[W] = {}, v[W];
-        FfnRow<W> r;
-        ffn_row<W, EPI>(p, m, n, r);
+        const FfnRow<W> r = {};
 #pragma unroll 4
         for (int c = 0; c < p.splits; ++c) {
             const float *q = p.part + ((int64_t)c * p.M + m) * width + n;
@@ -37,9 +35,7 @@ template <int KIND, int EPI> __global__ void __launch_bounds__(256) ffn_finish_k
 
 template <int KIND> static int launch_finish(const FfnArgs &a, int epi, hipStream_t stream) {
     const int64_t groups = ((int64_t)((a.N + 7) / 8) * a.M + 255) / 256;
-    auto fn = epi == FFN_GATE   ? ffn_finish_kernel<KIND, FFN_GATE>
-              : epi == FFN_GRAD ? ffn_finish_kernel<KIND, FFN_GRAD>
-                                : ffn_finish_kernel<KIND, FFN_STORE>;
+    auto fn = epi == FFN_GATE ? ffn_finish_kernel<KIND, FFN_GATE> : ffn_finish_kernel<KIND, FFN_STORE>;
     hipLaunchKernelGGL(fn, dim3((unsigned)(groups < 16384 ? groups : 16384)), dim3(256), 0, stream, a);
     ANN_HIP_TRY(hipGetLastError());
     return ANN_OK;
@@ -190,12 +186,6 @@ static bool ffn_stride(const char *name, int64_t ld, int64_t width) {
     }
     return true;
 }
-static bool overlap(const void *a, int64_t rows_a, int64_t ld_a, int64_t w_a, const void *b, int64_t rows_b, int64_t ld_b,
-                    int64_t w_b, size_t e) {
-    const uintptr_t a0 = (uintptr_t)a, a1 = a0 + (size_t)((rows_a - 1) * ld_a + w_a) * e;
-    const uintptr_t b0 = (uintptr_t)b, b1 = b0 + (size_t)((rows_b - 1) * ld_b + w_b) * e;
-    return a0 < b1 && b0 < a1;
-}
 static bool ffn_workspace(const void *ws, size_t have, size_t need, int *rc) {
     if (!ws || (uintptr_t)ws % 256) {
         set_error("workspace_dev must not be null and must be 256-byte aligned");
@@ -241,7 +231,7 @@ int ann_gated_ffn(const void *x_dev, int64_t ld_x, const void *w_in_dev, const v
         !ffn_array("b_in_dev", b_in_dev, e, true) || !ffn_array("b_out_dev", b_out_dev, e, true) ||
         !ffn_array("pre_dev", pre_dev, 4, true) || !ffn_stride("ld_x", ld_x, d_in) || !ffn_stride("ld_out", ld_out, d_out))
         return rc;
-    if (overlap(x_dev, M, ld_x, d_in, out_dev, M, ld_out, d_out, e)) {
+    if (rows_overlap(x_dev, ld_x, d_in, out_dev, ld_out, d_out, M, e)) {
         set_error("out_dev must not overlap x_dev");
         return rc;
     }
@@ -306,8 +296,8 @@ int ann_gated_ffn_backward(const void *dout_dev, int64_t ld_dout, const void *x_
         !ffn_array("w_out_dev", w_out_dev, e, false) || !ffn_stride("ld_dout", ld_dout, d_out) ||
         !ffn_stride("ld_x", ld_x, d_in) || (dx_dev && !ffn_stride("ld_dx", ld_dx, d_in)))
         return rc;
-    if (dx_dev && (overlap(dx_dev, M, ld_dx, d_in, dout_dev, M, ld_dout, d_out, e) ||
-                   overlap(dx_dev, M, ld_dx, d_in, x_dev, M, ld_x, d_in, e))) {
+    if (dx_dev && (rows_overlap(dx_dev, ld_dx, d_in, dout_dev, ld_dout, d_out, M, e) ||
+                   rows_overlap(dx_dev, ld_dx, d_in, x_dev, ld_x, d_in, M, e))) {
         set_error("dx_dev must not overlap dout_dev or x_dev");
         return rc;
     }

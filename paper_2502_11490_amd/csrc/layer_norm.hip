@@ -474,6 +474,11 @@ static bool ln_sizes(int64_t M, int32_t d, int32_t dtype) {
     }
     return true;
 }
+static bool ln_apart(const char *names, const void *a, int64_t ld_a, const void *b, int64_t ld_b, int64_t M, int32_t d, int32_t dtype) {
+    if ((a == b && ld_a == ld_b) || !rows_overlap(a, ld_a, d, b, ld_b, d, M, elem_bytes(dtype))) return true;
+    set_error("%s must be the same rows or have none in common", names);
+    return false;
+}
 static bool ln_rows(const char *name, const void *p, int64_t ld, int64_t M, int32_t d, int32_t dtype) {
     if (!p || (uintptr_t)p % elem_bytes(dtype) || ld < d || ld > (int64_t)1 << 40) {
         set_error("%s must not be null, must be aligned to its elements and have a row stride of at least d = %d (got %lld)",
@@ -498,6 +503,7 @@ int ann_layer_norm(const void *x_dev, int64_t ld_x, const void *gamma_dev, const
     }
     if (M == 0) return ANN_OK;
     if (!ln_rows("x_dev", x_dev, ld_x, M, d, dtype) || !ln_rows("out_dev", out_dev, ld_out, M, d, dtype)) return ANN_EINVAL;
+    if (!ln_apart("x_dev and out_dev", x_dev, ld_x, out_dev, ld_out, M, d, dtype)) return ANN_EINVAL;
     if (((uintptr_t)gamma_dev | (uintptr_t)beta_dev) % elem_bytes(dtype) || ((uintptr_t)mean_dev | (uintptr_t)rstd_dev) % 4) {
         set_error("gamma_dev, beta_dev, mean_dev and rstd_dev must be aligned to their elements");
         return ANN_EINVAL;
@@ -527,7 +533,9 @@ int ann_layer_norm_backward(const void *dout_dev, int64_t ld_dout, const void *x
         return rc == ANN_OK && dbeta_dev ? launch_zero(dbeta_dev, d, dtype, s) : rc;
     }
     if (!ln_rows("dout_dev", dout_dev, ld_dout, M, d, dtype) || !ln_rows("x_dev", x_dev, ld_x, M, d, dtype) ||
-        (dx_dev && !ln_rows("dx_dev", dx_dev, ld_dx, M, d, dtype)))
+        (dx_dev && (!ln_rows("dx_dev", dx_dev, ld_dx, M, d, dtype) ||
+                    !ln_apart("dout_dev and dx_dev", dout_dev, ld_dout, dx_dev, ld_dx, M, d, dtype) ||
+                    !ln_apart("x_dev and dx_dev", x_dev, ld_x, dx_dev, ld_dx, M, d, dtype))))
         return ANN_EINVAL;
     if (!mean_dev || !rstd_dev || ((uintptr_t)mean_dev | (uintptr_t)rstd_dev) % 4) {
         set_error("mean_dev and rstd_dev must not be null and must be aligned to their elements");

@@ -53,6 +53,17 @@ template <typename T> __device__ __forceinline__ void store_floats(T *p, int lef
 inline bool row_dtype(int32_t dtype) { return dtype == ANN_F32 || dtype == ANN_BF16 || dtype == ANN_F16; }
 inline size_t elem_bytes(int32_t dtype) { return dtype == ANN_F32 ? 4 : 2; }
 
+// Whether two arrays of M rows share an element: their extents do, and they are not columns side by side of one array.
+inline bool rows_overlap(const void *a, int64_t ld_a, int64_t width_a, const void *b, int64_t ld_b, int64_t width_b, int64_t M,
+                         size_t e) {
+    const uintptr_t a0 = (uintptr_t)a, b0 = (uintptr_t)b;
+    const uintptr_t a1 = a0 + (size_t)((M - 1) * ld_a + width_a) * e, b1 = b0 + (size_t)((M - 1) * ld_b + width_b) * e;
+    if (a0 >= b1 || b0 >= a1) return false;
+    if (ld_a != ld_b) return true;
+    const uintptr_t line = (uintptr_t)ld_a * e, from = (b0 + (a0 / line + 1) * line - a0) % line;  // b's column, from a's
+    return !(from >= (uintptr_t)width_a * e && from + (uintptr_t)width_b * e <= line);
+}
+
 // rows.hip: first[c] (c < n) and second[c - n] = sum over P of part[p][c], in the order of p, rounded once to dtype; part
 // [P][2 n] fp32, either result may be null
 int launch_sum_two(const float *part, int64_t P, int64_t n, void *first, void *second, int dtype, hipStream_t stream);

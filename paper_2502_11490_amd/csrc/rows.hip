@@ -4,17 +4,18 @@
 
 namespace gmpgr {
 
-// Adds the parts of 32 columns, one thread a column and eighth of the parts; the eighths are joined in order.
+// Adds the parts of 32 columns, one thread a column and 32nd of the parts, which are joined in order.  (With eighths of 500
+// parts, whose reads follow each other, 6.3 us instead of 4.)
 template <int KIND>
 __device__ __forceinline__ void sum_columns(const float *__restrict__ part, int64_t P, int64_t width, int64_t first_col,
                                             int64_t n, typename ElemOf<KIND>::type *first,
                                             typename ElemOf<KIND>::type *second) {
-    __shared__ float s[8][32];
+    __shared__ float s[32][32];
     const int c = threadIdx.x & 31, y = threadIdx.x >> 5;
     const int64_t col = first_col + c;
     float acc = 0.f;
     if (col < width) {
-        const int64_t p0 = P * y / 8, p1 = P * (y + 1) / 8;
+        const int64_t p0 = P * y / 32, p1 = P * (y + 1) / 32;
 #pragma unroll 8
         for (int64_t p = p0; p < p1; ++p) acc += part[p * width + col];
     }
@@ -22,14 +23,14 @@ __device__ __forceinline__ void sum_columns(const float *__restrict__ part, int6
     __syncthreads();
     if (y == 0 && col < width) {
 #pragma unroll
-        for (int i = 1; i < 8; ++i) acc += s[i][c];
+        for (int i = 1; i < 32; ++i) acc += s[i][c];
         typename ElemOf<KIND>::type *out = col < n ? first : second;
         if (out) out[col < n ? col : col - n] = (typename ElemOf<KIND>::type)acc;
     }
 }
 
 template <int KIND>
-__global__ void __launch_bounds__(256)
+__global__ void __launch_bounds__(1024)
 sum_two_kernel(const float *__restrict__ part, int64_t P, int64_t n, typename ElemOf<KIND>::type *first,
                typename ElemOf<KIND>::type *second) {
     sum_columns<KIND>(part, P, 2 * n, (int64_t)blockIdx.x * 32, n, first, second);
@@ -38,11 +39,11 @@ sum_two_kernel(const float *__restrict__ part, int64_t P, int64_t n, typename El
 int launch_sum_two(const float *part, int64_t P, int64_t n, void *first, void *second, int dtype, hipStream_t stream) {
     const dim3 grid((unsigned)((2 * n + 31) / 32));
     if (dtype == ANN_F32)
-        hipLaunchKernelGGL(sum_two_kernel<ANN_F32>, grid, dim3(256), 0, stream, part, P, n, (float *)first, (float *)second);
+        hipLaunchKernelGGL(sum_two_kernel<ANN_F32>, grid, dim3(1024), 0, stream, part, P, n, (float *)first, (float *)second);
     else if (dtype == ANN_BF16)
-        hipLaunchKernelGGL(sum_two_kernel<ANN_BF16>, grid, dim3(256), 0, stream, part, P, n, (__bf16 *)first, (__bf16 *)second);
+        hipLaunchKernelGGL(sum_two_kernel<ANN_BF16>, grid, dim3(1024), 0, stream, part, P, n, (__bf16 *)first, (__bf16 *)second);
     else
-        hipLaunchKernelGGL(sum_two_kernel<ANN_F16>, grid, dim3(256), 0, stream, part, P, n, (_Float16 *)first, (_Float16 *)second);
+        hipLaunchKernelGGL(sum_two_kernel<ANN_F16>, grid, dim3(1024), 0, stream, part, P, n, (_Float16 *)first, (_Float16 *)second);
     ANN_HIP_TRY(hipGetLastError());
     return ANN_OK;
 }
@@ -91,7 +92,7 @@ template <int KIND> __global__ void __launch_bounds__(256) column_slices_kernel(
     }
 }
 
-template <int KIND> __global__ void __launch_bounds__(256) sum_column_parts_kernel(ColumnSums sums, int first_groups) {
+template <int KIND> __global__ void __launch_bounds__(1024) sum_column_parts_kernel(ColumnSums sums, int first_groups) {
     const bool second = (int)blockIdx.x >= first_groups;
     const ColumnSums::Item &a = sums.item[second];
     sum_columns<KIND>(a.part, a.parts, a.n, (int64_t)(blockIdx.x - (second ? first_groups : 0)) * 32, a.n,
@@ -116,7 +117,7 @@ template <int KIND> static int launch_column_sums_of(const ColumnSums &sums, int
         ANN_HIP_TRY(hipGetLastError());
     }
     const int64_t first = (sums.item[0].n + 31) / 32, all = first + (sums.n > 1 ? (sums.item[1].n + 31) / 32 : 0);
-    hipLaunchKernelGGL(sum_column_parts_kernel<KIND>, dim3((unsigned)all), dim3(256), 0, stream, sums, (int)first);
+    hipLaunchKernelGGL(sum_column_parts_kernel<KIND>, dim3((unsigned)all), dim3(1024), 0, stream, sums, (int)first);
     ANN_HIP_TRY(hipGetLastError());
     return ANN_OK;
 }

@@ -34,6 +34,24 @@ def test_layer_norm_refuses(lib, bad):
     assert _ln(lib, **bad) == -1 and lib.ann_last_error()
 
 
+def test_rows_that_lie_on_each_other_are_refused_and_columns_side_by_side_are_not(lib):
+    """4 fp32 rows of 8 about address 4096.  No device is reached: where the rows are in order a later check refuses."""
+    at = lambda elements: ctypes.c_void_p(4096 + 4 * elements)  # noqa: E731
+    assert _ln(lib, x=at(0), out=at(1)) == -1 and b"in common" in lib.ann_last_error()
+    assert _ln(lib, x=at(0), ld=16, out=at(4), ld_out=16) == -1 and b"in common" in lib.ann_last_error()
+    assert _ln(lib, x=at(0), ld=16, out=at(0), ld_out=24) == -1 and b"in common" in lib.ann_last_error()
+    assert _ln(lib, x=at(0), ld=16, out=at(8), ld_out=16, gamma=ctypes.c_void_p(4097)) == -1 and b"aligned" in lib.ann_last_error()
+    assert _ln(lib, x=at(8), ld=16, out=at(0), ld_out=16, gamma=ctypes.c_void_p(4097)) == -1 and b"aligned" in lib.ann_last_error()
+    assert _ln(lib, x=at(0), out=at(0), gamma=ctypes.c_void_p(4097)) == -1 and b"aligned" in lib.ann_last_error()
+    assert _ln_back(lib, dout=at(0), x=at(1 << 16), dx=at(1)) == -1 and b"dout_dev and dx_dev" in lib.ann_last_error()
+    assert _ln_back(lib, dout=at(0), x=at(1 << 16), dx=at((1 << 16) + 8)) == -1 and b"x_dev and dx_dev" in lib.ann_last_error()
+    assert lib.ann_dropout(at(0), None, at(1), 16, 0, 0.5, 1, 0, None, None) == -1 and b"overlap" in lib.ann_last_error()
+    assert lib.ann_dropout(at(64), at(0), at(1), 16, 0, 0.5, 1, 0, None, None) == -1 and b"overlap" in lib.ann_last_error()
+    assert _ffn(lib, x=at(0), ld=16, out=at(4), ld_out=16) == -1 and b"overlap" in lib.ann_last_error()
+    assert _ffn(lib, x=at(0), ld=16, out=at(8), ld_out=16, ws=None) == -1 and b"workspace" in lib.ann_last_error()
+    assert _ffn(lib, x=at(24), ld=16, out=at(0), ld_out=16, ws=None) == -1 and b"workspace" in lib.ann_last_error()
+
+
 def test_layer_norm_of_no_rows(lib):
     assert _ln(lib, x=None, out=None, M=0) == 0
 
