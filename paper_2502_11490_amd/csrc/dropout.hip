@@ -7,6 +7,8 @@
 // e % 8 is >= t = round(65536 p), and kept elements are scaled by 65536 / (65536 - t): with the probability rounded to
 // 2^-16 the scale is exact for the probability that is drawn.  A dropped element is selected away, never multiplied,
 // so infinities and NaN in dropped places leave nothing.
+//   Bound by memory: 16 bits an element make one block of 20 wide products serve 8 elements.  32768 x 4096 bf16: with
+// residual 144 us, 5.6 TB/s; without 96 us, 5.6 TB/s.
 #include <math.h>
 
 #include "philox.h"

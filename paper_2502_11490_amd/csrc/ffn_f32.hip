@@ -7,6 +7,8 @@
 // floats apart, and gives a lane its 4 in one read of 16 bytes (16 lanes on 16 different sets of banks); one whose rows
 // are contiguous lies as [k][row], lines 8 floats longer than the tile, so that the two halves' k lie on the two halves of
 // the banks.
+// 8192 x 1024 x 4096: 610 us, 113 TFLOP/s, in tiles of 128, 674 in tiles of 64; those keep the last round of middling products
+// short: 2048 x 1300 x 256 (FFN_GRAD) 33 us against 41.
 #include "ffn.h"
 
 namespace gmpgr {

@@ -44,8 +44,9 @@ template <int KIND> static int launch_finish(const FfnArgs &a, int epi, hipStrea
 // The cut that a simple account says is fastest: rounds of workgroups over 256 compute units, each of which holds a_unit of
 // them, a round as many steps of 64 k as a slice has and a start and an end; a last round that leaves units with fewer
 // workgroups is that much shorter; and for slices the writing and reading of the parts and one more launch.  Fitted to
-// measured products: of 8192 x 8192 x 2048 (FFN_GRAD) 442 us in tiles of 256, 472 in tiles of 128; 4096 x 2048 x 512
-// (FFN_GATE) 32 and 28; 4096 x 2048 x 2048 (FFN_STORE) 52 and 34; 8192 x 2048 x 16384 (FFN_STORE) 448 and 550.
+// measured products: of 8192 x 8192 x 2048 (FFN_GRAD) 449 us in tiles of 256, 478 in tiles of 128; 8192 x 8192 x 2048
+// (FFN_GATE) 562 and 793, 4096 x 2048 x 2048 63 and 68; 4096 x 2048 x 2048 (FFN_STORE) 40 in two slices of k and 35; 8192 x
+// 2048 x 16384 442 and 569.
 struct FfnTileCost {
     int rows, cols, a_unit;
     double step, ends[3];  // microseconds of 64 k, of the start and the end by epilogue, with a_unit of them at work

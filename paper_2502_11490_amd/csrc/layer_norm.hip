@@ -7,7 +7,10 @@
 // (packed, as it lies in memory), the variance is summed over the deviations from the mean that the registers give, and
 // the row is written from them.  A team of threads owns a row: 2^t lanes of a wave for narrow rows, a workgroup for wide
 // ones; a team takes one row after the other, so that gamma, beta and the sums of the columns' gradients stay in
-// registers.  Rows that no team's registers hold are read three times (out of the caches, mostly).
+// registers, and the next row is on its way while one is worked on.  Rows that no team's registers hold are read three times
+// (out of the caches, mostly).
+//   16384 x 4096 bf16: forward 47 us, 5.7 TB/s (without the row ahead 54); gradient 80 + 5 us, 5.0 TB/s (without 107); two
+// workgroups a compute unit in the gradient keep the column sums, 2 d floats each, at 4 % of its traffic.
 #include "rows.h"
 
 namespace gmpgr {
