@@ -474,7 +474,7 @@ int ann_dropout(const void *x_dev, const void *residual_dev, void *out_dev, int6
  *   pre_dev   [M][2 * d_hidden] fp32          : gate and up before the activation, written for the gradient; NULL where none is taken
  * Products are accumulated in fp32.  In the 16-bit types h is rounded to the type, as the operand of the second product
  * (with up to 8 rows it keeps twice the type's bits); gate and up are not rounded.  fp16 overflows where the formula's h or out do.
- * M >= 0 (0: nothing is done), M < 2^31; every width 1 .. 2^20.
+ * M >= 0 (0: nothing is done), M <= 2^29; every width 1 .. 2^20.
  * workspace_dev: ann_gated_ffn_workspace_bytes with the same sizes (0 on invalid ones).
  */
 enum { ANN_SILU = 0, ANN_GELU = 1, ANN_SIGMOID = 2, ANN_RELU = 3 };

@@ -165,9 +165,11 @@ static Rows ffn_rows(int dtype, const void *p, int64_t ld, int64_t rows, int64_t
 }
 
 static bool ffn_sizes(int64_t M, int32_t D, int32_t F, int32_t O, int32_t dtype) {
+    // M is the k of the weights' gradients, which the kernels count in 32 bits up to three steps past its end, and with 2^29
+    // rows in tiles of 64 a launch has 2^31 threads
     const int32_t w = 1 << 20;
-    if (M < 0 || M > 0x7fffffffll || D < 1 || D > w || F < 1 || F > w || O < 1 || O > w || !row_dtype(dtype)) {
-        set_error("need 0 <= M < 2^31, widths 1 .. 2^20, dtype ANN_F32, ANN_BF16 or ANN_F16 (got M=%lld, %d, %d, %d, dtype %d)",
+    if (M < 0 || M > (1 << 29) || D < 1 || D > w || F < 1 || F > w || O < 1 || O > w || !row_dtype(dtype)) {
+        set_error("need 0 <= M <= 2^29, widths 1 .. 2^20, dtype ANN_F32, ANN_BF16 or ANN_F16 (got M=%lld, %d, %d, %d, dtype %d)",
                   (long long)M, D, F, O, dtype);
         return false;
     }

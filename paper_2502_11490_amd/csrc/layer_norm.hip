@@ -184,7 +184,7 @@ ln_forward_any_kernel(const typename ElemOf<KIND>::type *x, int64_t ld_x,
 }
 
 // The gradient.  Sums over a team's rows of dout xh and dout stay in registers; the teams of a workgroup are joined in
-// LDS, part[workgroup][2][d] goes to memory, and sum_parts_kernel adds the workgroups in order.
+// LDS, part[workgroup][2][d] goes to memory, and sum_two_kernel adds the workgroups in order.
 template <int KIND, int LANES, int NV>
 __global__ void __launch_bounds__(LANES ? LANES : 256)
 ln_backward_kernel(const typename ElemOf<KIND>::type *dout, int64_t ld_dout, const typename ElemOf<KIND>::type *x,

@@ -123,6 +123,18 @@ def test_gated_ffn_backward_workspace(lib):
     assert _ffn_back(lib, wb=lib.ann_gated_ffn_backward_workspace_bytes(4, 8, 16, 8, 0) - 1) == -5
 
 
+@pytest.mark.parametrize("dtype", [0, 1, 3])
+def test_gated_ffn_takes_no_more_rows_than_its_kernels_count(lib, dtype):
+    """A reduction over M rows is counted in 32 bits, some steps past its end."""
+    for M in ((1 << 29) + 1, (1 << 31) - 64, (1 << 31) - 1):
+        assert lib.ann_gated_ffn_workspace_bytes(M, 1, 1, 1, dtype) == 0
+        assert lib.ann_gated_ffn_backward_workspace_bytes(M, 1, 1, 1, dtype) == 0
+        assert _ffn(lib, M=M, dtype=dtype) == -1 and b"2^29" in lib.ann_last_error()
+        assert _ffn_back(lib, M=M, dtype=dtype) == -1 and b"2^29" in lib.ann_last_error()
+    assert lib.ann_gated_ffn_workspace_bytes(1 << 29, 1, 1, 1, dtype) > 0
+    assert lib.ann_gated_ffn_backward_workspace_bytes(1 << 29, 1, 1, 1, dtype) > 0
+
+
 def test_binding_refuses():
     x, w = torch.zeros(4, 8), torch.zeros(8)
     for f in (lambda: ann.ann_layer_norm(x),                                     # not on a device
