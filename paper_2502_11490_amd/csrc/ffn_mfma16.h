@@ -21,6 +21,7 @@
 #pragma once
 
 #include "ffn.h"
+#include "keys.h"  // wave_lds_fence
 
 namespace gmpgr {
 
@@ -229,12 +230,14 @@ __global__ void __launch_bounds__(256, BM == 256 ? 1 : 2) ffn_mfma16_kernel(FfnA
         constexpr bool INSIDE = decltype(inside)::value;
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
+            if (half) wave_lds_fence();  // other lanes have read the first half's sums
 #pragma unroll
             for (int i = 0; i < MT / 2; ++i)
 #pragma unroll
                 for (int j = 0; j < NT; ++j)
                     *(f32x4 *)(mine + (i * 16 + (lane & 15)) * WN + ((j * 4 + (lane >> 4)) ^ (lane & 15)) * 4) =
                         acc[half * (MT / 2) + i][j];
+            wave_lds_fence();  // what a lane reads others have written
             const int64_t m_first = m0 + wm + half * HALF + lane_row;
             FfnRow<4> row[AHEAD][2], next[AHEAD][2];
             auto fetch = [&](int r0) {
