@@ -56,7 +56,7 @@ __device__ __forceinline__ void ffn_act_each(int act, const float *z, float *val
     } else if (act == ANN_GELU) {
 #pragma unroll
         for (int i = 0; i < W; ++i) {
-            const float cdf = 0.5f * (1.0f + erff(z[i] * 0.70710678118654752f));
+            const float cdf = 0.5f * erfcf(z[i] * -0.70710678118654752f);  // as (1 + erf) / 2 it would end at z = -5
             value[i] = z[i] * cdf;
             if (SLOPE) slope[i] = cdf + z[i] * (0.39894228040143268f * ffn_exp<KIND>(-0.5f * z[i] * z[i]));
         }
