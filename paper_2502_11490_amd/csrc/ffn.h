@@ -49,9 +49,13 @@ __device__ __forceinline__ void ffn_act_each(int act, const float *z, float *val
         const bool silu = act == ANN_SILU;
 #pragma unroll
         for (int i = 0; i < W; ++i) {
-            const float sig = ffn_sigmoid<KIND>(z[i]), t = sig * (1.0f - sig);
+            const float sig = ffn_sigmoid<KIND>(z[i]);
             value[i] = silu ? z[i] * sig : sig;
-            if (SLOPE) slope[i] = silu ? sig + z[i] * t : t;
+            if (SLOPE) {
+                // 1 - sig = exp(-z) sig, which keeps its bits where sig is near 1; exp(-z) overflows where sig is 0
+                const float e = ffn_exp<KIND>(-z[i]), t = sig * (e < __builtin_inff() ? e * sig : 1.0f);
+                slope[i] = silu ? sig + z[i] * t : t;
+            }
         }
     } else if (act == ANN_GELU) {
 #pragma unroll

@@ -38,11 +38,8 @@ def test_values_in_the_tails(act, dtype, M):
     bo.assert_close(got, want, want.abs() * _relative(z) + h * bo.half_step(want, TYPES[dtype]))
 
 
-SLOPES = [ann.ANN_SILU, ann.ANN_GELU]
-
-
 @pytest.mark.parametrize("dtype", TYPES)
-@pytest.mark.parametrize("act", SLOPES, ids=[NAMES[a] for a in SLOPES])
+@pytest.mark.parametrize("act", NAMES, ids=NAMES.values())
 def test_slopes_in_the_tails(act, dtype):
     z, x, w_in, w_out, b_in = _one_unit(TYPES[dtype])
     pre = torch.cat((z, torch.ones_like(z)), 1).float()
