@@ -473,7 +473,9 @@ int ann_dropout(const void *x_dev, const void *residual_dev, void *out_dev, int6
  *               ANN_SIGMOID, ANN_RELU
  *   pre_dev   [M][2 * d_hidden] fp32          : gate and up before the activation, written for the gradient; NULL where none is taken
  * Products are accumulated in fp32.  In the 16-bit types h is rounded to the type, as the operand of the second product
- * (with up to 8 rows it keeps twice the type's bits); gate and up are not rounded.  fp16 overflows where the formula's h or out do.
+ * (with up to 8 rows it keeps twice the type's bits, as far as the type's range goes); gate and up are not rounded.  So a row's
+ * result depends on the number of rows of its call, by roundings: from 8 rows to 9 by that of h, else by the order of fp32 sums.
+ * fp16 overflows where the formula's h or out do.
  * M >= 0 (0: nothing is done), M <= 2^29; every width 1 .. 2^20.
  * workspace_dev: ann_gated_ffn_workspace_bytes with the same sizes (0 on invalid ones).
  */
@@ -489,7 +491,9 @@ int ann_gated_ffn(const void *x_dev, int64_t ld_x, const void *w_in_dev, const v
  *     dh = dout w_out, dgate = dh * up * act'(gate), dup = dh * act(gate), dx = [dgate | dup] w_in,
  *     dw_in = [dgate | dup]^T x, dw_out = dout^T h, db_in = column sums of [dgate | dup], db_out = column sums of dout.
  * In the 16-bit types dgate, dup and h are rounded to the type, as operands of the products; nothing else is rounded
- * before the results (db_in sums dgate and dup before their rounding).  ANN_RELU has slope 0 at 0.
+ * before the results (db_in sums dgate and dup before their rounding).  In fp16 a dgate or dup beyond 65504 is infinite, dx and
+ * dw_in with it, and one below 2^-14 loses bits, below 2^-25 all: dout must be scaled so that they lie between.  ANN_RELU has
+ * slope 0 at 0.
  * dout_dev [M][d_out]; dx_dev [M][d_in] must not overlap dout_dev or x_dev; dx_dev, dw_in_dev, db_in_dev, dw_out_dev,
  * db_out_dev have the shapes of what they are gradients of, NULL = not wanted.  With M = 0 the parameters' gradients are zeroed.
  * workspace_dev: ann_gated_ffn_backward_workspace_bytes with the same sizes (0 on invalid ones).
