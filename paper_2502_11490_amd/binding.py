@@ -651,7 +651,8 @@ def ann_quantize_e4m3(src: torch.Tensor, scale: float = 1.0, out: Optional[torch
 #
 # Tensors of one call lie on one device; the call goes to that device's current stream, or to `stream`, a stream of it.
 # Results and workspaces that the call makes belong to the stream it goes to; that its inputs are there, and stay until it
-# has read them, is the caller's to see to.  Gradients are calls of their own: these functions leave no trace in autograd.
+# has read them, is the caller's to see to.  Gradients are calls of their own: these functions leave no trace in autograd, also
+# where a tensor requires gradients.
 
 _ROW_CODE = {torch.float32: ANN_F32, torch.bfloat16: ANN_BF16, torch.float16: ANN_F16}
 
@@ -727,7 +728,7 @@ def _row_workspace(workspace: Optional[torch.Tensor], need: int, x: torch.Tensor
 def ann_layer_norm(x: torch.Tensor, gamma: Optional[torch.Tensor] = None, beta: Optional[torch.Tensor] = None,
                    eps: float = 1e-5, save: bool = False, out: Optional[torch.Tensor] = None, stream=None):
     """Layer norm over the last dimension of x [..., d]; gamma, beta [d] of x's type (None = ones, zeros).  `out` may be
-    x.  With save=True (out, mean, rstd), the last two fp32 [rows], for ann_layer_norm_backward."""
+    x.  With save=True (out, mean, rstd), the last two fp32 [rows], for ann_layer_norm_backward; autograd does not see the call."""
     place = _place(x, stream)
     if place is not None:
         with place:
@@ -791,7 +792,8 @@ def ann_dropout(x: torch.Tensor, p: float, seed: int, draw: int = 0, residual: O
                 out: Optional[torch.Tensor] = None, draw_dev: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """residual + dropout of x (None = no residual), the choice a pure function of (seed, draw, element): the gradient
     of x is ann_dropout(dout, p, seed, draw).  Contiguous tensors of one shape; `out` may be x or residual.  draw_dev
-    (one int64 on the device) is added to `draw` when the kernel runs: the replays of a recorded call draw anew."""
+    (one int64 on the device) is added to `draw` when the kernel runs: the replays of a recorded call draw anew.  Autograd does
+    not see the call."""
     place = _place(x, stream)
     if place is not None:
         with place:
@@ -838,7 +840,7 @@ def ann_gated_ffn(x: torch.Tensor, w_in: torch.Tensor, w_out: torch.Tensor, b_in
                   out: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None, stream=None):
     """(act(gate) * up) w_out^T + b_out with [gate | up] = x w_in^T + b_in: x [..., d_in], w_in [2 * d_hidden][d_in] (the gate's
     rows first), w_out [d_out][d_hidden], all of one type.  With save=True (out, pre), pre [rows][2 * d_hidden] fp32, for
-    ann_gated_ffn_backward."""
+    ann_gated_ffn_backward; autograd does not see the call."""
     place = _place(x, stream)
     if place is not None:
         with place:
