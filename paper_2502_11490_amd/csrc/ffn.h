@@ -234,9 +234,15 @@ template <int KIND> int launch_ffn16(const FfnProduct &p, int tile, hipStream_t 
 int launch_ffn32(const FfnProduct &p, int cols, hipStream_t stream);                      // ffn_f32.hip
 
 // ffn_few.hip: the same for few rows, both operands' k contiguous, any alignment; FFN_STORE and FFN_GATE, no slices.
-// Up to how many rows that is the faster kernel: with N = 8192 gate columns and K = 2048 in bf16 16 us against 22 for 32
-// rows and 21 against 22 for 64; with N = 2048 and K = 8192 (h in two parts) 10 us against 16 for one row, 24 against 16
-// for 16 (too few workgroups, that read x over and over); in fp32 34 against 32 and 68 against 21 for 64.
+// Up to how many rows they are taken, with the kernels' times (few rows / tiles and the joining of their slices, us) at the
+// lines, for 2048 -> 2 x 8192 -> 2048, 1024 -> 2 x 4096 -> 1024 and 512 -> 2 x 2048 -> 128, four blocks' weights in turn:
+//   FFN_GATE, 16 bits, 64: 23 / 24, 10 / 14 and 6 / 10 with 64 rows; more have no kernel here.
+//   FFN_GATE, fp32, 16: 36 / 84, 11 / 28 and 7 / 18 with 16 rows; more would gain too (with 64 rows 61 / 82, 21 / 29, 12 / 19), but
+//     have no kernel here.
+//   FFN_STORE, 16 bits, 8, up to where h comes in two parts: 14 / 16, 8 / 10 and 6 / 9 with 8 rows.  With h in one part the lead
+//     ends later: 15 / 16, 8 / 11 and 5 / 9 with 9 rows, 17 / 16, 9 / 11 and 6 / 9 with 16.
+//   FFN_STORE, fp32, 16: with 8 rows 24 / 31, 10 / 13 and 6 / 11, with 9 33 / 30, 15 / 13 and 9 / 13, with 16 37 / 30, 17 / 13 and
+//     10 / 13: from 9 rows on narrow outputs gain what wide ones lose.
 constexpr int ffn_few(int kind, int epi) { return kind == ANN_F32 ? 16 : epi == FFN_GATE ? 64 : 8; }
 int launch_ffn_few(const FfnProduct &p, hipStream_t stream);
 

@@ -8,8 +8,8 @@
 // (8) rows in 4 (2) slices of a step: four times the workgroups, so that few columns still occupy every compute unit, and of
 // the 16 x 16 sums the blocks on the diagonal are added.  h comes in two 16-bit parts, its rounding and what that leaves
 // over: the instructions are idle anyway, and out is then as near as from an fp32 h.  Several steps' loads are on their way together.
-// One bf16 row through 2048 -> 2 x 8192 (67 MB): 13.3 us, 5.0 TB/s; 8192 -> 2048 (34 MB): 9.7 us, 3.5 TB/s (without slices
-// 11.6 us, with h in one part 8.5 us).
+// One bf16 row through 2048 -> 2 x 8192 (67 MB): 13 to 14 us, 4.7 to 5.1 TB/s; 8192 -> 2048 (34 MB): 9.3 to 10 us, 3.3 to 3.6
+// TB/s (without slices 11.6 us, with h in one part 8.5 us).  In fp32: 31 us (134 MB, 4.3 TB/s) and 16 us (67 MB, 4.3 TB/s).
 #include "ffn.h"
 
 namespace gmpgr {

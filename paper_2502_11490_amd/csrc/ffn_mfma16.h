@@ -15,6 +15,7 @@
 //   bf16 products M x N x K, in tiles of 256 and, forced, of 128: 8192 x 2048 x 8192 243 us (1.13 PFLOP/s) and 287; with w as
 // [k][row], 8192 x 2048 x 16384, 442 us (1.24) and 569; with both as [k][row], 16384 x 2048 x 8192, 473 us (1.16) and 556;
 // FFN_GATE 8192 x 2 8192 x 2048 562 us (0.98) and 793; FFN_GRAD 8192 x 8192 x 2048, whose epilogue moves 0.94 GB, 449 and 478.
+// (Averages of ten passes; other cards and runs are up to 4 % slower.)
 // With the loop's loads into LDS taken out the first three are 197, 406 and 444 us: the matrix instructions bound them, under
 // that load's clock, and the loads add 6 to 23 %.  Two workgroups of the 128 tile share a compute unit: 4096 x 2048 x 2048
 // 35 us, where the 256 tile has to cut k in two to occupy the units, 40 us and the joining.

@@ -46,7 +46,9 @@ template <int KIND> static int launch_finish(const FfnArgs &a, int epi, hipStrea
 // workgroups is that much shorter; and for slices the writing and reading of the parts and one more launch.  Fitted to
 // measured products: of 8192 x 8192 x 2048 (FFN_GRAD) 449 us in tiles of 256, 478 in tiles of 128; 8192 x 8192 x 2048
 // (FFN_GATE) 562 and 793, 4096 x 2048 x 2048 63 and 68; 4096 x 2048 x 2048 (FFN_STORE) 40 in two slices of k and 35; 8192 x
-// 2048 x 16384 442 and 569.
+// 2048 x 16384 442 and 569.  It is up to 20 % low for products that end inside a tile and a round: of 1537 x 2 x 2731 x 1003 in
+// fp16 (FFN_GATE) it says 40 us, which take 50 (and of the other tile 44, which is as near), of 1537 x 2731 x 777 (FFN_GRAD)
+// 34, which take 43, of 2048 x 1300 x 256 in fp32 (FFN_GRAD) 27, which take 33.
 struct FfnTileCost {
     int rows, cols, a_unit;
     double step, ends[3];  // microseconds of 64 k, of the start and the end by epilogue, with a_unit of them at work
